@@ -310,6 +310,171 @@ typedef struct {
 int lvspec_kv_commit(const lvspec_commit_args* args, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Paged KV cache in 8 bits (beyond the paper, which leaves the cache to the implementation): half the
+ * bytes of a step's attention, and sequences of a batch that take blocks from one pool as they grow.
+ *
+ * Block = LVSPEC_PAGE_TOKENS (64) consecutive positions of a sequence.  For one layer:
+ *   k_pool   e4m3 [n_blocks, Hkv, 64, 128]     keys of a complete block, a token per row
+ *   v_pool   e4m3 [n_blocks, Hkv, 128, 64]     values of a complete block, a channel per row
+ *   k_scale, v_scale   fp32 [n_blocks, Hkv]    value = code * scale; the scale is the smallest power of
+ *                                              two s >= 2^-60 with max |x| <= 448 s over the block's
+ *                                              finite values; codes are rounded to nearest even, what
+ *                                              is not finite becomes NaN
+ *   k_tail, v_tail     bf16 [B, Hkv, 128, 128] ring of LVSPEC_TAIL_ROWS rows per sequence: position p at
+ *                                              row p % 128
+ * and, shared by the layers, a table int32 [B, table_cols]: entry j is the block of positions 64 j ..
+ * 64 j + 63.  With L committed positions the L / 64 complete blocks are in the pool; the L % 64 open
+ * rows and the draft rows behind them (positions L .. L+gamma-1) are in the ring.  So a value is
+ * rounded to 8 bits once, with its block's scale, whatever pieces the rows arrived in.
+ * All arrays are contiguous; pools and tails 16-byte aligned.  Every layer has its own arrays; where one
+ * call serves n_layers they lie one after the other ([n_layers, n_blocks, ...], [n_layers, B, ...]).
+ *
+ * A decode loop:  plan(n_new = prompt rows) and append per layer; then per step plan(draft = 1, n_new =
+ * reserve = draft rows), append or a plain copy of the draft rows into the ring, attention, acceptance,
+ * commit of all layers.  Only device memory is read, so steps can be captured into a graph.
+ * ------------------------------------------------------------------------------------------- */
+#define LVSPEC_PAGE_TOKENS 64
+#define LVSPEC_TAIL_ROWS 128
+#define LVSPEC_PAGED_MAX_B 4096
+#define LVSPEC_PAGED_MAX_BLOCKS (1 << 24)
+#define LVSPEC_SLOT_NONE (-1)       /* slot of a row that is stored nowhere */
+#define LVSPEC_SLOT_TAIL (-2)       /* slot of ring row r of sequence b: LVSPEC_SLOT_TAIL - (128 b + r) */
+
+typedef struct {
+  int32_t B, Hkv, D;                /* D must be 128; B <= 4096 */
+  int32_t n_blocks;                 /* blocks of the pool, 1 .. 2^24 */
+  void* k_pool;                     /* DEVICE */
+  void* v_pool;                     /* DEVICE */
+  float* k_scale;                   /* DEVICE */
+  float* v_scale;                   /* DEVICE */
+  void* k_tail;                     /* DEVICE */
+  void* v_tail;                     /* DEVICE */
+} lvspec_paged_cache;
+
+/* ---------------------------------------------------------------------------------------------
+ * Block tables and slot maps from request lengths.  For request b, with len = kv_len[b] committed
+ * rows, n = n_new[b] rows to come (packed one request behind the other), end = len + n and
+ * done = (draft ? len : end) / 64 blocks that are complete behind them:
+ *     cu_rows[b]  = rows of the requests before b; cu_rows[B] = all rows (both at most max_rows)
+ *     need        = (end + reserve) / 64;  grow = max(need - held[b], 0)
+ *     granted[b]  = need <= table_cols, the rows fit into max_rows and, open, into the ring
+ *                   (end - 64 done <= 128), and (grow == 0 or the queue holds enough for the grow of all
+ *                   requests up to b: first come, first served, nobody overtakes)
+ *     new_held[b] = granted ? need : held[b];  table[b, held .. need-1] = blocks from the queue's front,
+ *                   in the order of requests and columns;  blocks table[b, need .. held-1] of a granted
+ *                   request that shrinks go to the queue's end and are given out from the next call on
+ *     row t of request b (cu_rows[b] <= t < cu_rows[b+1]), position p = len + t - cu_rows[b]:
+ *         row_seq[t] = b, row_pos[t] = p, slots[t] = 64 table[b, p / 64] + p % 64 where p < 64 done,
+ *         else LVSPEC_SLOT_TAIL - (128 b + p % 128); LVSPEC_SLOT_NONE for a request not granted
+ *     rows cu_rows[B] .. max_rows-1: slot LVSPEC_SLOT_NONE, row_seq and row_pos -1
+ * The queue is a ring int32 [n_blocks] of free blocks: state = {index of the first, number}.  At the
+ * start state = {0, n_blocks}, queue = 0 .. n_blocks-1, held = 0.  A finished request is one with
+ * kv_len = n_new = 0.  Nothing is changed in place but table entries at and behind held[b] and queue
+ * entries behind its end, so a repeated call gives the same answer.  Lengths below 0 count as 0.
+ * Errors: LVSPEC_EINVAL for NULL / out-of-range arguments, new_held aliasing held or new_state state.
+ * ------------------------------------------------------------------------------------------- */
+typedef struct {
+  int32_t B;                        /* requests, 1 .. 4096 */
+  int32_t table_cols;               /* >= 1 */
+  int32_t n_blocks;
+  int32_t max_rows;                 /* entries of slots, row_seq and row_pos, 0 .. 2^28 */
+  int32_t reserve;                  /* rows beyond end that the table is to have blocks for, 0 .. 2^20 */
+  int32_t draft;                    /* 1: the rows are drafts, all of them go to the ring */
+  const int32_t* kv_len;            /* DEVICE [B] */
+  const int32_t* n_new;             /* DEVICE [B] */
+  const int32_t* held;              /* DEVICE [B] blocks of the requests' tables */
+  const int32_t* state;             /* DEVICE [2] */
+  int32_t* queue;                   /* DEVICE [n_blocks], changed behind its end */
+  int32_t* table;                   /* DEVICE [B, table_cols], changed from held[b] on */
+  int32_t* granted;                 /* DEVICE out [B]: 1 or 0 */
+  int32_t* new_held;                /* DEVICE out [B]; must not alias held */
+  int32_t* new_state;               /* DEVICE out [2]; must not alias state */
+  int32_t* cu_rows;                 /* DEVICE out [B + 1] */
+  int32_t* slots;                   /* DEVICE out [max_rows] */
+  int32_t* row_seq;                 /* DEVICE out [max_rows] */
+  int32_t* row_pos;                 /* DEVICE out [max_rows] */
+} lvspec_paged_plan_args;
+
+int lvspec_paged_plan(const lvspec_paged_plan_args* args, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * New rows of one layer into the cache, by the maps of lvspec_paged_plan.  Rows with a ring slot are
+ * copied there.  A row with a pool slot that is the last of its block (slot % 64 == 63) completes it: the
+ * block's 64 rows, packed ones and, for positions before the call, those of the ring, are rounded to
+ * 8 bits with their scale.  Slots of a call are distinct.  Rows whose slot names no block of the pool
+ * or no row of the ring are not stored.  k, v must not overlap the cache.
+ * Errors: LVSPEC_EINVAL for NULL / misaligned / out-of-range arguments, LVSPEC_EUNSUPPORTED for D != 128.
+ * ------------------------------------------------------------------------------------------- */
+typedef struct {
+  lvspec_paged_cache cache;
+  int32_t n_rows;                   /* packed rows, 0 .. 2^28 */
+  const void* k;                    /* DEVICE bf16 [n_rows, Hkv, 128] */
+  const void* v;                    /* DEVICE bf16 [n_rows, Hkv, 128] */
+  int64_t k_sr, k_sh, v_sr, v_sh;   /* strides: row, kv head */
+  const int32_t* slots;             /* DEVICE [n_rows] */
+  const int32_t* row_seq;           /* DEVICE [n_rows] */
+  const int32_t* row_pos;           /* DEVICE [n_rows] */
+  const int32_t* cu_rows;           /* DEVICE [B + 1] */
+} lvspec_paged_append_args;
+
+int lvspec_paged_append(const lvspec_paged_append_args* args, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Verification attention over the paged cache: as lvspec_verify_attn, with the keys and values of
+ * complete blocks as the cache holds them (scale * code, exactly) and the ring's rows in bf16.  The
+ * draft rows must be in the ring.  kv_len[b] is clamped to [0, 64 table_cols + 63] by the kernels.  A
+ * table entry below L / 64 that names no block of the pool holds no key: its positions are left out.
+ * Where a sequence's keys are cut, and with that the rounding of its bf16 probabilities (a relative 2e-3
+ * of the result), follows from the lengths of all sequences and the shapes.
+ * Errors: as lvspec_verify_attn.
+ * ------------------------------------------------------------------------------------------- */
+typedef struct {
+  lvspec_paged_cache cache;
+  int32_t gamma, Hq;                /* Hq % Hkv == 0; 1 <= gamma <= 32 */
+  const void* q;                    /* DEVICE bf16 [B, gamma, Hq, 128] */
+  int64_t q_sb, q_sg, q_sh;         /* strides of q: batch, draft row, head */
+  const int32_t* table;             /* DEVICE [B, table_cols]; may be NULL when table_cols == 0 */
+  int32_t table_cols;
+  const int32_t* kv_len;            /* DEVICE [B] */
+  const int32_t* vis_begin;         /* DEVICE [B] or NULL: first position of the video span */
+  const int32_t* vis_end;           /* DEVICE [B] or NULL: one past its last position */
+  const uint32_t* draft_mask;       /* HOST [gamma] or NULL, as in lvspec_attn_args */
+  float scale;                      /* score scale; 0 = 1/sqrt(D) */
+  void* out;                        /* DEVICE bf16 [B, gamma, Hq, 128] */
+  int64_t o_sb, o_sg, o_sh;         /* strides of out */
+  float* lse;                       /* DEVICE fp32 [B, Hq, gamma] or NULL */
+  float* vis_mass;                  /* DEVICE fp32 [B, Hq, gamma] or NULL (needs vis_begin/end) */
+  void* workspace;                  /* DEVICE */
+  size_t workspace_bytes;
+} lvspec_paged_attn_args;
+
+size_t lvspec_verify_attn_paged_workspace(const lvspec_paged_attn_args* args);
+int lvspec_verify_attn_paged(const lvspec_paged_attn_args* args, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Committing a verified step, as lvspec_kv_commit: tau = accept_len of the kept chain, new_len[b] =
+ * kv_len[b] + tau; when kept > 0 the ring rows of positions kv_len[b] + kept*chain_len + i become those
+ * of kv_len[b] + i, i < tau; and a block that becomes complete is rounded to 8 bits into block
+ * table[b, kv_len[b] / 64], in every layer.  A sequence whose block has no place there (column behind the
+ * table, or an entry outside the pool: it was not granted) or whose kv_len is out of range is left as it
+ * is, new_len[b] = kv_len[b].
+ * Errors: LVSPEC_EINVAL for NULL / out-of-range arguments or new_len aliasing kv_len.
+ * ------------------------------------------------------------------------------------------- */
+typedef struct {
+  lvspec_paged_cache cache;         /* of the first layer */
+  int32_t n_layers;                 /* 1 .. 65535 */
+  int32_t n_branches, chain_len;    /* as in lvspec_commit_args */
+  const int32_t* table;             /* DEVICE [B, table_cols] */
+  int32_t table_cols;
+  const int32_t* kv_len;            /* DEVICE [B] */
+  const int32_t* accept_len;        /* DEVICE [B * n_branches] */
+  const int32_t* best_branch;       /* DEVICE [B] or NULL */
+  int32_t* new_len;                 /* DEVICE out [B]; must not alias kv_len */
+} lvspec_paged_commit_args;
+
+int lvspec_paged_commit(const lvspec_paged_commit_args* args, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Diagnostics: how the three verify calls would be launched for the given shapes (no paper
  * passage behind this one: it reports the library's own launch planning, for tuning and tests).
  * Any of the argument pointers may be NULL; its fields of *out are then left untouched.  Only

@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -27,6 +27,8 @@ STATIC_SCRATCH_BYTES = 16 << 20
 REJECT, EXACT, LOOSE, SHIFT, GATED = 0, 1, 2, 3, 4
 RULE_VISUAL, RULE_ENTROPY_GATE, RULE_ENTROPY_WINDOW = 0, 1, 2
 MAX_GAMMA, MAX_TOPK, MAX_TOPN = 16, 16, 1024
+PAGE_TOKENS, TAIL_ROWS = 64, 128          # of the paged cache in 8 bits
+SLOT_NONE, SLOT_TAIL = -1, -2
 
 
 class AttnArgs(C.Structure):
@@ -100,6 +102,54 @@ class CommitArgs(C.Structure):
     ]
 
 
+class PagedCacheStruct(C.Structure):
+    _fields_ = [
+        ("B", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32), ("n_blocks", C.c_int32),
+        ("k_pool", C.c_void_p), ("v_pool", C.c_void_p),
+        ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+        ("k_tail", C.c_void_p), ("v_tail", C.c_void_p),
+    ]
+
+
+class PagedPlanArgs(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("B", "table_cols", "n_blocks", "max_rows", "reserve", "draft")] + [
+        (n, C.c_void_p) for n in ("kv_len", "n_new", "held", "state", "queue", "table", "granted", "new_held",
+                                  "new_state", "cu_rows", "slots", "row_seq", "row_pos")]
+
+
+class PagedAppendArgs(C.Structure):
+    _fields_ = [
+        ("cache", PagedCacheStruct), ("n_rows", C.c_int32),
+        ("k", C.c_void_p), ("v", C.c_void_p),
+        ("k_sr", C.c_int64), ("k_sh", C.c_int64), ("v_sr", C.c_int64), ("v_sh", C.c_int64),
+        ("slots", C.c_void_p), ("row_seq", C.c_void_p), ("row_pos", C.c_void_p), ("cu_rows", C.c_void_p),
+    ]
+
+
+class PagedAttnArgs(C.Structure):
+    _fields_ = [
+        ("cache", PagedCacheStruct), ("gamma", C.c_int32), ("Hq", C.c_int32),
+        ("q", C.c_void_p), ("q_sb", C.c_int64), ("q_sg", C.c_int64), ("q_sh", C.c_int64),
+        ("table", C.c_void_p), ("table_cols", C.c_int32), ("kv_len", C.c_void_p),
+        ("vis_begin", C.c_void_p), ("vis_end", C.c_void_p),
+        ("draft_mask", C.POINTER(C.c_uint32)),
+        ("scale", C.c_float),
+        ("out", C.c_void_p), ("o_sb", C.c_int64), ("o_sg", C.c_int64), ("o_sh", C.c_int64),
+        ("lse", C.c_void_p), ("vis_mass", C.c_void_p),
+        ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+    ]
+
+
+class PagedCommitArgs(C.Structure):
+    _fields_ = [
+        ("cache", PagedCacheStruct), ("n_layers", C.c_int32),
+        ("n_branches", C.c_int32), ("chain_len", C.c_int32),
+        ("table", C.c_void_p), ("table_cols", C.c_int32),
+        ("kv_len", C.c_void_p), ("accept_len", C.c_void_p), ("best_branch", C.c_void_p),
+        ("new_len", C.c_void_p),
+    ]
+
+
 class PlanInfo(C.Structure):
     _fields_ = [(n, C.c_int32) for n in (
         "attn_rows_padded", "attn_row_chunks", "attn_splits", "rel_splits", "rel_stage_bytes",
@@ -129,11 +179,19 @@ _lib.lvspec_hv_prepare.argtypes = [C.POINTER(HvArgs), C.c_void_p]
 _lib.lvspec_verify_attn_static.restype = C.c_int
 _lib.lvspec_verify_attn_static.argtypes = [C.POINTER(AttnArgs), C.c_void_p]
 
+for _name, _t in (("paged_plan", PagedPlanArgs), ("paged_append", PagedAppendArgs),
+                  ("verify_attn_paged", PagedAttnArgs), ("paged_commit", PagedCommitArgs)):
+    getattr(_lib, f"lvspec_{_name}").restype = C.c_int
+    getattr(_lib, f"lvspec_{_name}").argtypes = [C.POINTER(_t), C.c_void_p]
+_lib.lvspec_verify_attn_paged_workspace.restype = C.c_size_t
+_lib.lvspec_verify_attn_paged_workspace.argtypes = [C.POINTER(PagedAttnArgs)]
+
 EXPORTS = ["lvspec_hv_prepare", "lvspec_verify_attn_static", "lvspec_status_string", "lvspec_version", "lvspec_last_hip_error", "lvspec_n_loose",
            "lvspec_verify_attn_workspace", "lvspec_verify_attn",
            "lvspec_visual_relevance_workspace", "lvspec_visual_relevance",
            "lvspec_loose_accept_workspace", "lvspec_loose_accept", "lvspec_kv_commit",
-           "lvspec_describe_plan"]
+           "lvspec_describe_plan", "lvspec_paged_plan", "lvspec_paged_append",
+           "lvspec_verify_attn_paged_workspace", "lvspec_verify_attn_paged", "lvspec_paged_commit"]
 
 
 class LvspecError(RuntimeError):
@@ -429,3 +487,203 @@ def describe_plan(attn: Optional[AttnArgs] = None, rel: Optional[RelArgs] = None
                 (name.startswith("acc_") and accept is not None)):
             out[name] = int(getattr(info, name))
     return out
+
+
+# ------------------------------------------------------------------ paged cache in 8 bits
+class PagedCache(NamedTuple):
+    """The arrays of one layer, or of several with a leading dimension (include/lvspec.h says what
+    they hold).  Pools: float8_e4m3fn or uint8."""
+    k_pool: torch.Tensor      # [n_blocks, Hkv, 64, 128]
+    v_pool: torch.Tensor      # [n_blocks, Hkv, 128, 64]
+    k_scale: torch.Tensor     # fp32 [n_blocks, Hkv]
+    v_scale: torch.Tensor
+    k_tail: torch.Tensor      # bf16 [B, Hkv, 128, 128]
+    v_tail: torch.Tensor
+
+    def layer(self, i: int) -> "PagedCache":
+        return PagedCache(*[x[i] for x in self])
+
+
+def alloc_paged_cache(B, Hkv, n_blocks, device, layers: Optional[int] = None) -> PagedCache:
+    lead = () if layers is None else (layers,)
+
+    def new(shape, dtype):
+        return torch.zeros(lead + shape, dtype=dtype, device=device)
+
+    return PagedCache(
+        new((n_blocks, Hkv, PAGE_TOKENS, 128), torch.float8_e4m3fn),
+        new((n_blocks, Hkv, 128, PAGE_TOKENS), torch.float8_e4m3fn),
+        new((n_blocks, Hkv), torch.float32), new((n_blocks, Hkv), torch.float32),
+        new((B, Hkv, TAIL_ROWS, 128), torch.bfloat16), new((B, Hkv, TAIL_ROWS, 128), torch.bfloat16))
+
+
+def alloc_paged_state(B, n_blocks, table_cols, device) -> dict:
+    """What the plan of a batch starts from: every block free, nobody holds one."""
+    def new(*shape):
+        return torch.zeros(shape, dtype=torch.int32, device=device)
+
+    state = new(2)
+    state[1] = n_blocks
+    return dict(held=new(B), state=state, queue=torch.arange(n_blocks, dtype=torch.int32, device=device),
+                table=new(B, table_cols) - 1)
+
+
+def alloc_paged_plan(B, max_rows, device) -> dict:
+    """The outputs of paged_plan."""
+    shapes = dict(granted=B, new_held=B, new_state=2, cu_rows=B + 1, slots=max_rows, row_seq=max_rows,
+                  row_pos=max_rows)
+    return {k: torch.empty((n,), dtype=torch.int32, device=device) for k, n in shapes.items()}
+
+
+def _dense(t, dtype, shape, *also):
+    assert t.is_cuda and t.dtype in (dtype, *also) and t.is_contiguous() and tuple(t.shape) == tuple(shape), (
+        t.device, t.dtype, tuple(t.shape))
+    return t.data_ptr()
+
+
+def _call_on(device, fn, a, stream):
+    """The call with the tensors' device current, which need not be the caller's."""
+    if device.index == torch.cuda.current_device():
+        _check(fn(C.byref(a), _stream(stream)))
+    else:
+        with torch.cuda.device(device):
+            _check(fn(C.byref(a), _stream(stream)))
+
+
+def _cache_struct(cache: PagedCache, lead=()) -> PagedCacheStruct:
+    n = len(lead)
+    n_blocks, Hkv = cache.k_pool.shape[n:n + 2]
+    B = cache.k_tail.shape[n]
+    f8, bf = torch.float8_e4m3fn, torch.bfloat16
+    s = PagedCacheStruct()
+    s.B, s.Hkv, s.D, s.n_blocks = B, Hkv, 128, n_blocks
+    s.k_pool = _dense(cache.k_pool, f8, (*lead, n_blocks, Hkv, PAGE_TOKENS, 128), torch.uint8)
+    s.v_pool = _dense(cache.v_pool, f8, (*lead, n_blocks, Hkv, 128, PAGE_TOKENS), torch.uint8)
+    s.k_scale = _dense(cache.k_scale, torch.float32, (*lead, n_blocks, Hkv))
+    s.v_scale = _dense(cache.v_scale, torch.float32, (*lead, n_blocks, Hkv))
+    s.k_tail = _dense(cache.k_tail, bf, (*lead, B, Hkv, TAIL_ROWS, 128))
+    s.v_tail = _dense(cache.v_tail, bf, (*lead, B, Hkv, TAIL_ROWS, 128))
+    return s
+
+
+def paged_plan_args(kv_len, n_new, held, queue, state, table, *, outs, max_rows, reserve=0,
+                    draft=False) -> PagedPlanArgs:
+    i32 = torch.int32
+    B, cols = table.shape
+    a = PagedPlanArgs()
+    a.B, a.table_cols, a.n_blocks = B, cols, queue.numel()
+    a.max_rows, a.reserve, a.draft = int(max_rows), int(reserve), 1 if draft else 0
+    a.kv_len, a.n_new, a.held = (_dense(x, i32, (B,)) for x in (kv_len, n_new, held))
+    a.state, a.queue, a.table = _dense(state, i32, (2,)), _dense(queue, i32, queue.shape), _dense(table, i32, (B, cols))
+    sizes = dict(granted=B, new_held=B, new_state=2, cu_rows=B + 1, slots=max_rows, row_seq=max_rows, row_pos=max_rows)
+    for name, n in sizes.items():
+        setattr(a, name, _dense(outs[name], i32, (n,)))
+    return a
+
+
+def paged_plan(kv_len, n_new, held, queue, state, table, *, max_rows, reserve=0, draft=False, outs=None,
+               stream=None) -> dict:
+    """lvspec_paged_plan.  kv_len, n_new, held int32 [B]; queue int32 [n_blocks], state int32 [2], table
+    int32 [B, cols] (queue and table are changed).  Returns granted, new_held, new_state, cu_rows, slots,
+    row_seq, row_pos; new_held and new_state are held and state of the next call."""
+    if outs is None:
+        outs = alloc_paged_plan(table.shape[0], max_rows, table.device)
+    a = paged_plan_args(kv_len, n_new, held, queue, state, table, outs=outs, max_rows=max_rows, reserve=reserve,
+                        draft=draft)
+    _call_on(table.device, _lib.lvspec_paged_plan, a, stream)
+    return outs
+
+
+def paged_append_args(cache: PagedCache, k, v, plan) -> PagedAppendArgs:
+    i32 = torch.int32
+    a = PagedAppendArgs()
+    a.cache = _cache_struct(cache)
+    n = k.shape[0]
+    assert k.is_cuda and v.is_cuda and k.dtype == torch.bfloat16 and v.dtype == torch.bfloat16 and k.shape == v.shape
+    assert k.shape[1:] == (a.cache.Hkv, 128) and k.stride(-1) == 1 and v.stride(-1) == 1
+    a.n_rows, a.k, a.v = n, k.data_ptr(), v.data_ptr()
+    # (torch gives any stride to a dimension of one)
+    a.k_sr, a.k_sh, a.v_sr, a.v_sh = [x.stride(d) if x.shape[d] > 1 else max(x.stride(d), 128)
+                                      for x in (k, v) for d in (0, 1)]
+    a.slots, a.row_seq, a.row_pos = (_dense(plan[x], i32, (n,)) for x in ("slots", "row_seq", "row_pos"))
+    a.cu_rows = _dense(plan["cu_rows"], i32, (a.cache.B + 1,))
+    return a
+
+
+def paged_append(cache: PagedCache, k, v, plan, *, stream=None) -> None:
+    """lvspec_paged_append.  k, v bf16 [n_rows, Hkv, 128], a packed row for every entry of the plan's
+    maps (plan: what paged_plan returned, with max_rows = n_rows)."""
+    a = paged_append_args(cache, k, v, plan)
+    _call_on(k.device, _lib.lvspec_paged_append, a, stream)
+
+
+def verify_attn_paged_args(q, cache: PagedCache, table, kv_len, *, out, vis_begin=None, vis_end=None,
+                           draft_mask=None, scale=0.0, lse=None, vis_mass=None) -> PagedAttnArgs:
+    i32 = torch.int32
+    a = PagedAttnArgs()
+    a.cache = _cache_struct(cache)
+    B, gamma, Hq, D = q.shape
+    assert q.is_cuda and out.is_cuda and q.dtype == torch.bfloat16 and out.dtype == torch.bfloat16
+    assert out.shape == q.shape
+    assert B == a.cache.B and D == 128 and q.stride(-1) == 1 and out.stride(-1) == 1
+    a.gamma, a.Hq = gamma, Hq
+    a.q, (a.q_sb, a.q_sg, a.q_sh) = q.data_ptr(), q.stride()[:3]
+    a.table, a.table_cols = _dense(table, i32, (B, table.shape[1])), table.shape[1]
+    a.kv_len = _dense(kv_len, i32, (B,))
+    for name, t in (("vis_begin", vis_begin), ("vis_end", vis_end)):
+        setattr(a, name, None if t is None else _dense(t, i32, (B,)))
+    if draft_mask is not None:
+        assert len(draft_mask) == gamma
+        a._keep = a.draft_mask = (C.c_uint32 * gamma)(*[int(m) for m in draft_mask])
+    a.scale = float(scale)
+    a.out, (a.o_sb, a.o_sg, a.o_sh) = out.data_ptr(), out.stride()[:3]
+    for name, t in (("lse", lse), ("vis_mass", vis_mass)):
+        setattr(a, name, None if t is None else _dense(t, torch.float32, (B, Hq, gamma)))
+    return a
+
+
+def verify_attn_paged(q, cache: PagedCache, table, kv_len, *, vis_begin=None, vis_end=None, draft_mask=None,
+                      scale=0.0, out=None, return_lse=False, return_vis_mass=False, workspace=None,
+                      stream=None):
+    """lvspec_verify_attn_paged.  q bf16 [B,gamma,Hq,128], one layer's cache, table int32 [B,cols], kv_len
+    int32 [B].  Returns out, or (out, lse, vis_mass) when either extra is asked for."""
+    B, gamma, Hq, _ = q.shape
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    lse = q.new_empty((B, Hq, gamma), dtype=torch.float32) if return_lse else None
+    vm = q.new_empty((B, Hq, gamma), dtype=torch.float32) if return_vis_mass else None
+    a = verify_attn_paged_args(q, cache, table, kv_len, out=out, vis_begin=vis_begin, vis_end=vis_end,
+                               draft_mask=draft_mask, scale=scale, lse=lse, vis_mass=vm)
+    ws = _workspace(_lib.lvspec_verify_attn_paged_workspace(C.byref(a)), q, workspace)
+    a.workspace, a.workspace_bytes = ws.data_ptr(), ws.numel() * ws.element_size()
+    _call_on(q.device, _lib.lvspec_verify_attn_paged, a, stream)
+    if return_lse or return_vis_mass:
+        return out, lse, vm
+    return out
+
+
+def paged_commit_args(cache: PagedCache, table, kv_len, accept_len, chain_len, *, best_branch=None, n_branches=1,
+                      new_len) -> PagedCommitArgs:
+    i32 = torch.int32
+    layers = cache.k_pool.shape[0] if cache.k_pool.dim() == 5 else 1
+    a = PagedCommitArgs()
+    a.cache = _cache_struct(cache, (layers,) if cache.k_pool.dim() == 5 else ())
+    B = a.cache.B
+    a.n_layers, a.n_branches, a.chain_len = layers, int(n_branches), int(chain_len)
+    a.table, a.table_cols = _dense(table, i32, (B, table.shape[1])), table.shape[1]
+    a.kv_len, a.new_len = _dense(kv_len, i32, (B,)), _dense(new_len, i32, (B,))
+    a.accept_len = _dense(accept_len, i32, (B * max(1, int(n_branches)),))
+    a.best_branch = None if best_branch is None else _dense(best_branch, i32, (B,))
+    return a
+
+
+def paged_commit(cache: PagedCache, table, kv_len, accept_len, chain_len, *, best_branch=None, n_branches=1,
+                 new_len=None, stream=None):
+    """lvspec_paged_commit.  cache of one layer, or of all with a leading dimension; accept_len int32
+    [B*n_branches], best_branch int32 [B] (trees).  Returns new_len int32 [B]."""
+    if new_len is None:
+        new_len = torch.empty_like(kv_len)
+    a = paged_commit_args(cache, table, kv_len, accept_len, chain_len, best_branch=best_branch,
+                          n_branches=n_branches, new_len=new_len)
+    _call_on(table.device, _lib.lvspec_paged_commit, a, stream)
+    return new_len

@@ -13,8 +13,10 @@
 static __device__ __align__(256) unsigned char scratch[LVSPEC_STATIC_SCRATCH_BYTES];
 
 namespace {
-
 thread_local int g_last_hip_error = 0;
+}
+
+namespace lvspec {
 
 int hip_fail(hipError_t e) {
   g_last_hip_error = (int)e;
@@ -43,6 +45,13 @@ int num_compute_units() {
   (void)hipGetLastError();
   return 256;
 }
+
+}  // namespace lvspec
+
+namespace {
+
+using lvspec::hip_fail;
+using lvspec::num_compute_units;
 
 size_t round_up(size_t x, size_t m) { return (x + m - 1) / m * m; }
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }

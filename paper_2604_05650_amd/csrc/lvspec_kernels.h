@@ -7,7 +7,14 @@
 
 #include <atomic>
 
+#include "../../include/lvspec.h"
+
 namespace lvspec {
+
+// api.hip: the compute units of the current device (256 where none can be queried), and LVSPEC_EHIP with
+// the error kept for lvspec_last_hip_error
+int num_compute_units();
+int hip_fail(hipError_t e);
 
 // Raises a kernel's dynamic-LDS limit once per device.  The HIP call is idempotent, so threads
 // that race on a first launch may both make it; the per-device flag only saves later calls
@@ -213,5 +220,87 @@ struct CommitKernelArgs {
   int32_t* new_len;
 };
 hipError_t launch_kv_commit(const CommitKernelArgs& a, hipStream_t stream);
+
+// ---------------------------------------------------------------- paged cache in 8 bits
+struct PlanKernelArgs {
+  const int32_t* kv_len;
+  const int32_t* n_new;
+  const int32_t* held;
+  const int32_t* state;         // queue: index of its first block, number of blocks in it
+  int32_t* queue;               // [n_blocks]
+  int32_t* table;               // [B][cols]
+  int32_t* granted;
+  int32_t* new_held;
+  int32_t* new_state;
+  int32_t* cu_rows;             // [B + 1]
+  int32_t* slots;               // [max_rows]
+  int32_t* row_seq;
+  int32_t* row_pos;
+  int B, cols, n_blocks, max_rows, reserve, draft;
+};
+hipError_t launch_paged_plan(const PlanKernelArgs& a, hipStream_t stream);
+
+struct AppendKernelArgs {
+  const uint8_t* k;
+  const uint8_t* v;
+  int64_t k_sr, k_sh, v_sr, v_sh;      // bytes between rows / heads of the packed rows
+  const int32_t* slots;
+  const int32_t* row_seq;
+  const int32_t* row_pos;
+  const int32_t* cu_rows;
+  uint8_t* k8;
+  uint8_t* v8;
+  float* k_scale;
+  float* v_scale;
+  uint8_t* k_tail;
+  uint8_t* v_tail;
+  int n_rows, B, Hkv, n_blocks;
+};
+hipError_t launch_paged_append(const AppendKernelArgs& a, hipStream_t stream);
+
+struct PagedCommitKernelArgs {
+  uint8_t* k8;
+  uint8_t* v8;
+  float* k_scale;
+  float* v_scale;
+  uint8_t* k_tail;
+  uint8_t* v_tail;
+  const int32_t* table;
+  const int32_t* kv_len;
+  const int32_t* accept_len;
+  const int32_t* best_branch;   // optional
+  int32_t* new_len;
+  int B, Hkv, n_layers, n_branches, chain_len, n_blocks, cols;
+};
+hipError_t launch_paged_commit(const PagedCommitKernelArgs& a, hipStream_t stream);
+
+struct PagedAttnKernelArgs {
+  const uint16_t* q;
+  int64_t q_sb, q_sg, q_sh;
+  const uint8_t* k8;
+  const uint8_t* v8;
+  const float* k_scale;
+  const float* v_scale;
+  const uint8_t* k_tail;
+  const uint8_t* v_tail;
+  const int32_t* table;
+  const int32_t* kv_len;
+  int B, gamma, Hq, Hkv;
+  int G, R;                     // Hq / Hkv; query rows per kv head, ordered r = i * G + (h % G)
+  int rpad, n_rc;               // rows per row chunk, row chunks
+  int n_blocks, cols;
+  int n_wg;                     // workgroups that share the complete blocks
+  float scale_log2e;
+  const int32_t* vis_begin;     // nullptr = no span
+  const int32_t* vis_end;
+  uint16_t* out;
+  int64_t o_sb, o_sg, o_sh;
+  float* lse;
+  float* vis_mass;
+  float* ws;                    // records of rpad * 131 floats: n_wg + units of blocks, units of open rows
+  uint32_t draft_mask[32];
+};
+hipError_t launch_paged_attn(const PagedAttnKernelArgs& a, hipStream_t stream);
+int paged_attn_workgroups(int rows, int num_cu);   // n_wg for so many rows per chunk
 
 }  // namespace lvspec
