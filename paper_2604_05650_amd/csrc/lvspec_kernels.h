@@ -289,7 +289,8 @@ struct PagedAttnKernelArgs {
   int G, R;                     // Hq / Hkv; query rows per kv head, ordered r = i * G + (h % G)
   int rpad, n_rc;               // rows per row chunk, row chunks
   int n_blocks, cols;
-  int n_wg;                     // workgroups that share the complete blocks
+  int n_wg;                     // workgroups of the split kernel, a multiple of 8
+  int streams;                  // waves of a workgroup with tiles of their own (set by the launch)
   float scale_log2e;
   const int32_t* vis_begin;     // nullptr = no span
   const int32_t* vis_end;
@@ -297,10 +298,10 @@ struct PagedAttnKernelArgs {
   int64_t o_sb, o_sg, o_sh;
   float* lse;
   float* vis_mass;
-  float* ws;                    // records of rpad * 131 floats: n_wg + units of blocks, units of open rows
+  float* ws;                    // n_wg + units records of rpad * 131 floats
   uint32_t draft_mask[32];
 };
 hipError_t launch_paged_attn(const PagedAttnKernelArgs& a, hipStream_t stream);
-int paged_attn_workgroups(int rows, int num_cu);   // n_wg for so many rows per chunk
+int paged_attn_workgroups(int num_cu);   // n_wg
 
 }  // namespace lvspec

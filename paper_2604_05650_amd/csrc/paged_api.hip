@@ -45,11 +45,11 @@ int plan_paged_attn(const lvspec_paged_attn_args* a, PagedPlan* pl) {
   pl->n_rc = (pl->R + 63) / 64;
   pl->rpad = ((pl->R + pl->n_rc - 1) / pl->n_rc + 3) / 4 * 4;
   // tiles of the line, units and output rows are 32-bit numbers in the kernels
-  const int64_t units = (int64_t)c.B * c.Hkv * pl->n_rc;
-  if (units * (a->table_cols + 1) > (int64_t)1 << 30 || (int64_t)c.B * c.Hkv * pl->R > (int64_t)1 << 30)
+  const int64_t units = (int64_t)c.B * c.Hkv * pl->n_rc;   // (the open rows of a unit have eight places)
+  if (units * ((int64_t)a->table_cols + 8) > (int64_t)1 << 30 || (int64_t)c.B * c.Hkv * pl->R > (int64_t)1 << 30)
     return LVSPEC_EUNSUPPORTED;
-  pl->n_wg = lvspec::paged_attn_workgroups(pl->rpad, lvspec::num_compute_units());
-  pl->ws_bytes = (size_t)(pl->n_wg + 2 * units) * pl->rpad * 131 * sizeof(float);
+  pl->n_wg = lvspec::paged_attn_workgroups(lvspec::num_compute_units());
+  pl->ws_bytes = (size_t)(pl->n_wg + units) * pl->rpad * 131 * sizeof(float);
   return LVSPEC_OK;
 }
 

@@ -26,6 +26,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kMergeStride = 132;      // floats per row in the merge buffer (pad)
 constexpr float kNegBig = -1.0e30f;
+constexpr int kBufferWord = 0x00020000;      // last word of a buffer resource: raw, 32-bit data
 
 // eight e4m3 times 2^e as bf16 (exact)
 LVS_DEV u32x4 widen(uint32_t lo, uint32_t hi, float scale) {
@@ -36,41 +37,37 @@ LVS_DEV u32x4 widen(uint32_t lo, uint32_t hi, float scale) {
 }
 
 // ------------------------------------------------------------------------------ the line of tiles
-// Sequence b's tiles start at HR * (complete blocks of the sequences before it), HR = Hkv * n_rc units
-// each of full(b) tiles.  Every wave finds its place by itself: sequences in groups of 64, one per lane.
-struct Line {
-  int total;           // tiles of the line
-  int per;             // tiles of a stretch
-};
+// The units, sequence by sequence (HR = Hkv * n_rc each), lie one behind the other on a line: a unit's tiles of
+// 64 keys, then kOpenTiles places for its open rows, which take about as long as so many tiles.  The line is
+// cut into equal stretches, one per workgroup, short ones of whole rounds (a tile per stream); who has the first of the open
+// rows' places does them.  Every wave finds its place by itself.
+constexpr int kOpenTiles = 8;
+constexpr int kWholeRounds = 32;
 
-LVS_DEV int wave_scan(int x, int lane) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(x, d, 64);
-    x += lane >= d ? y : 0;
-  }
+LVS_DEV int wave_scan(int x) {               // inclusive sum over the lanes
+  auto add = [&](uint32_t y) { x += (int)y; };
+  add(dpp_move<0x111, 0xf>(0u, (uint32_t)x));    // row_shr 1, 2, 4, 8
+  add(dpp_move<0x112, 0xf>(0u, (uint32_t)x));
+  add(dpp_move<0x114, 0xf>(0u, (uint32_t)x));
+  add(dpp_move<0x118, 0xf>(0u, (uint32_t)x));
+  add(dpp_move<0x142, 0xa>(0u, (uint32_t)x));    // row_bcast 15, 31
+  add(dpp_move<0x143, 0xc>(0u, (uint32_t)x));
   return x;
 }
+LVS_DEV int last_lane(int x) { return __builtin_amdgcn_readlane(x, 63); }
 
-LVS_DEV int full_blocks(const PagedAttnKernelArgs& p, int b) {
-  return b < p.B ? paged_len(p.kv_len[b], p.cols) >> kPageShift : 0;
-}
+LVS_DEV int full_blocks(const PagedAttnKernelArgs& p, int b) { return paged_len(p.kv_len[b], p.cols) >> kPageShift; }
 
-template <int KS>
-LVS_DEV Line line_of(const PagedAttnKernelArgs& p, int lane) {
-  int sum = 0;
-  for (int b0 = 0; b0 < p.B; b0 += 64) sum += full_blocks(p, b0 + lane);
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
-  Line l;
-  l.total = __builtin_amdgcn_readfirstlane(sum) * p.Hkv * p.n_rc;
-  // whole rounds of the streams: a stretch of 4 k + 1 tiles takes as long as one of 4 (k + 1)
-  const int rounds = (l.total + p.n_wg * KS - 1) / (p.n_wg * KS);
-  l.per = (rounds > 0 ? rounds : 1) * KS;
-  return l;
+// places of a sequence's unit on the line
+LVS_DEV int unit_places(const PagedAttnKernelArgs& p, int b) { return b < p.B ? full_blocks(p, b) + kOpenTiles : 0; }
+
+LVS_DEV int stretch_len(const PagedAttnKernelArgs& p, int total) {
+  const int each = (int)((uint32_t)(total + p.n_wg - 1) / (uint32_t)p.n_wg);
+  return each >= kWholeRounds ? each : (each + p.streams - 1) / p.streams * p.streams;
 }
 
 // ------------------------------------------------------------------------------ split
+// RG groups of NB * 16 rows by KS streams of tiles, a wave each.
 template <int NB, int RG, int KS>
 struct Shape {
   static constexpr int kWaves = RG * KS;
@@ -154,29 +151,38 @@ struct Segment {
   using W = Shape<NB, RG, KS>;
   const PagedAttnKernelArgs& p;
   uint8_t* smem;
-  int lane, wave, stream, rg, n16, g4;
+  int wave, stream, rg;
   u32x4 q[NB][4];          // channels 64 (c/2) + 16 g4 + 8 (c%2) .. +7 of row n16
-  int draft_row[NB];       // -1: no row
   RowState<NB> st;
   int vis_b, vis_e;
 
   LVS_DEV Segment(const PagedAttnKernelArgs& a, uint8_t* lds) : p(a), smem(lds) {
-    lane = threadIdx.x & 63;
     wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     stream = wave % KS;
     rg = wave / KS;
-    n16 = lane & 15;
-    g4 = lane >> 4;
   }
 
+  // The lane's number, row or token (n16) and quarter (g4).  Every part of a segment takes them anew: what
+  // follows from them would else be held in registers through the loop over the tiles.
+  struct Lane {
+    int lane, n16, g4;
+    LVS_DEV Lane() {
+      lane = threadIdx.x & 63;
+      asm volatile("" : "+v"(lane));
+      n16 = lane & 15;
+      g4 = lane >> 4;
+    }
+  };
+
   LVS_DEV void begin(int b, int h, int rc) {
+    const Lane me;
+    const int n16 = me.n16, g4 = me.g4;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       const int in = (rg * NB + nb) * 16 + n16, r = rc * p.rpad + in;
       const bool valid = in < p.rpad && r < p.R;
       const int rcl = r < p.R ? r : p.R - 1;
       const int qi = rcl / p.G;
-      draft_row[nb] = valid ? qi : -1;
       const uint16_t* qp = p.q + (int64_t)b * p.q_sb + (int64_t)qi * p.q_sg +
                            (int64_t)(h * p.G + (rcl - qi * p.G)) * p.q_sh;
 #pragma unroll
@@ -195,34 +201,43 @@ struct Segment {
 
   // tiles t0 .. t1-1 of a unit
   LVS_DEV void blocks(int b, int h, int t0, int t1) {
+    const Lane me;
+    const int lane = me.lane, n16 = me.n16, g4 = me.g4;
+    // (tiles that several waves read stay in the caches)
+    constexpr int kPolicy = RG == 1 ? kCopyStream : kCopyDefault;
     const int mine = (t1 - t0 - stream + KS - 1) / KS;
     if (mine <= 0) return;
     const int32_t* row = p.table + (int64_t)b * p.cols;
-    const int lane_at = (16 * (n16 >> 2) + (n16 & 3)) * 128 + 16 * g4;      // K: token, channel
-    const int turn_at = n16 * kPageTokens + 16 * g4;                          // V: channel, token
-    u32x4 k[8], v[8];
-    int ids = 0;
-    float ks = 0.f, vs = 0.f;
-    auto fetch = [&](int j0) {          // blocks and scales of the next 64 tiles, one per lane
+    const int k_at = (16 * (n16 >> 2) + (n16 & 3)) * 128 + 16 * g4;           // token, channel
+    const int v_at = n16 * kPageTokens + 16 * g4;                              // channel, token
+    // blocks and scales of 64 tiles, one per lane.  An entry that names no block of the pool is -1.
+    int ids;
+    float k_scales, v_scales;
+    auto fetch = [&](int j0) {
       const int t = t0 + stream + KS * (j0 + lane);
       ids = t < t1 ? row[t] : -1;
-      const bool there = (uint32_t)ids < (uint32_t)p.n_blocks;
-      const int64_t at = (int64_t)(there ? ids : 0) * p.Hkv + h;
-      ks = p.k_scale[at];
-      vs = p.v_scale[at];
-      ids = there ? ids : -1;
+      ids = (uint32_t)ids < (uint32_t)p.n_blocks ? ids : -1;
+      const int64_t at = (int64_t)max(ids, 0) * p.Hkv + h;
+      k_scales = p.k_scale[at];
+      v_scales = p.v_scale[at];
     };
-    auto load_k = [&](int id) {
-      const uint8_t* kp = p.k8 + ((int64_t)(id < 0 ? 0 : id) * p.Hkv + h) * kPageBytes + lane_at;
-#pragma unroll
-      for (int x = 0; x < 8; ++x)       // block x / 2 of 16 keys, channels 64 (x%2) ..
-        k[x] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kp + (x >> 1) * 512 + (x & 1) * 64));
+    // (no block: a buffer of no bytes, whose loads fetch nothing and give zero)
+    auto buffer = [&](const uint8_t* pool, int id) {
+      const int64_t at = ((int64_t)max(id, 0) * p.Hkv + h) * kPageBytes;
+      return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(pool + at), 0, id >= 0 ? kPageBytes : 0, kBufferWord);
     };
-    auto load_v = [&](int id) {
-      const uint8_t* vp = p.v8 + ((int64_t)(id < 0 ? 0 : id) * p.Hkv + h) * kPageBytes + turn_at;
+    u32x4 k[8], v[8];
+    auto load_k = [&](int id) {          // block x / 2 of 16 keys, channels 64 (x%2) ..
+      const auto from = buffer(p.k8, id);
 #pragma unroll
-      for (int db = 0; db < 8; ++db)
-        v[db] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vp + db * 1024));
+      for (int x = 0; x < 8; ++x)
+        k[x] = __builtin_amdgcn_raw_buffer_load_b128(from, k_at + (x >> 1) * 512 + (x & 1) * 64, 0, kPolicy);
+    };
+    auto load_v = [&](int id) {          // channels 16 x ..
+      const auto from = buffer(p.v8, id);
+#pragma unroll
+      for (int x = 0; x < 8; ++x)
+        v[x] = __builtin_amdgcn_raw_buffer_load_b128(from, v_at + (x & 3) * 1024, (x >> 2) * 4096, kPolicy);
     };
     fetch(0);
     int id = __builtin_amdgcn_readlane(ids, 0);
@@ -230,12 +245,10 @@ struct Segment {
     load_v(id);
     const float c = p.scale_log2e;
     for (int j = 0; j < mine; ++j) {
-      const float k_scale = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, ks), j & 63));
-      const float v_scale = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, vs), j & 63));
-      const bool there = id >= 0;
-      const bool more = j + 1 < mine;
-      if (more && ((j + 1) & 63) == 0) fetch(j + 1);
-      const int next = more ? __builtin_amdgcn_readlane(ids, (j + 1) & 63) : id;
+      const float k_scale = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, k_scales), j & 63));
+      const float v_scale = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v_scales), j & 63));
+      if (((j + 1) & 63) == 0) fetch(j + 1);
+      const int next = j + 1 < mine ? __builtin_amdgcn_readlane(ids, (j + 1) & 63) : -1;
       f32x4 s[NB][4];
 #pragma unroll
       for (int kb = 0; kb < 4; ++kb) {
@@ -249,8 +262,8 @@ struct Segment {
           for (int nb = 0; nb < NB; ++nb) s[nb][kb] = mfma16(a, q[nb][x], s[nb][kb]);
         }
       }
-      if (more) load_k(next);
-      if (there) {                      // (an entry that names no block of the pool: no key)
+      load_k(next);
+      if (id >= 0) {
         softmax_tile<NB, 4>(st, s, c);
         const int key0 = (t0 + stream + KS * j) * kPageTokens;
         span_mass<NB, 4>(st, s, key0, kPageTokens, vis_b, vis_e,
@@ -270,21 +283,25 @@ struct Segment {
             for (int nb = 0; nb < NB; ++nb) st.acc[nb][db] = mfma16(a, pr[nb][y], st.acc[nb][db]);
           }
       }
-      if (more) load_v(next);
+      load_v(next);
       id = next;
     }
   }
 
   // open rows: positions L / 64 * 64 .. L + gamma - 1, in pieces of 32 keys, one stream each
-  LVS_DEV void open_rows(int b, int h, int L) {
+  LVS_DEV void open_rows(int b, int h, int rc, int L) {
+    const Lane me;
+    const int n16 = me.n16, g4 = me.g4;
     const int base = L & ~(kPageTokens - 1);
     const int n = L - base + p.gamma;
     uint32_t rowmask[NB];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
+      const int in = (rg * NB + nb) * 16 + n16, r = rc * p.rpad + in;
+      const int draft_row = in < p.rpad && r < p.R ? r / p.G : -1;
       rowmask[nb] = 0u;
 #pragma unroll
-      for (int j = 0; j < 32; ++j) rowmask[nb] = draft_row[nb] == j ? p.draft_mask[j] : rowmask[nb];
+      for (int j = 0; j < 32; ++j) rowmask[nb] = draft_row == j ? p.draft_mask[j] : rowmask[nb];
       rowmask[nb] &= 0xffffffffu >> (32 - p.gamma);
     }
     const int64_t unit = ((int64_t)b * p.Hkv + h) * (kTailRows * kRowBytes);
@@ -385,6 +402,8 @@ struct Segment {
 
   // the streams' states into one record
   LVS_DEV void end(int rc, float* rec) {
+    const Lane me;
+    const int n16 = me.n16, g4 = me.g4;
     float* sm_m = reinterpret_cast<float*>(smem);          // [KS][kRows]
     float* sm_l = sm_m + KS * W::kRows;
     float* sm_v = sm_l + KS * W::kRows;
@@ -446,128 +465,149 @@ template <int NB, int RG, int KS>
 __global__ __launch_bounds__(64 * RG * KS, 2) void paged_attn_kernel(PagedAttnKernelArgs p) {
   extern __shared__ __align__(256) uint8_t smem[];
   Segment<NB, RG, KS> sg(p, smem);
-  const int HR = p.Hkv * p.n_rc;
-  const int units = p.B * HR;
-  if ((int)blockIdx.x < units) {                 // open rows first: they take the longest chain of steps
-    const int u = blockIdx.x, b = u / HR, hr = u - b * HR, h = hr / p.n_rc, rc = hr - h * p.n_rc;
-    const int L = paged_len(p.kv_len[b], p.cols);
-    sg.begin(b, h, rc);
-    sg.open_rows(b, h, L);
-    sg.end(rc, record_at(p, (int64_t)p.n_wg + units + u));
-    return;
-  }
-  const int i = blockIdx.x - units;
+  const int HR = p.Hkv * p.n_rc, lane = threadIdx.x & 63;
+  int places = unit_places(p, lane);
+  int upto = wave_scan(places), total = last_lane(upto);
+  for (int b0 = 64; b0 < p.B; b0 += 64) total += last_lane(wave_scan(unit_places(p, b0 + lane)));
+  total *= HR;
+  const int len = stretch_len(p, total);
+  const int used = (int)((uint32_t)(total + len - 1) / (uint32_t)len);     // stretches, at most n_wg
   // stretches that follow each other go to one XCD, which has the records of a unit in its L2
-  const int w = (i & 7) * (p.n_wg >> 3) + (i >> 3);
-  const Line line = line_of<KS>(p, sg.lane);
-  int at = w * line.per;
-  const int end = min(at + line.per, line.total);
-  int b0 = 0, before = 0;                        // sequences b0 .. b0+63 at hand, tiles / HR before them
+  const int each = (used + 7) >> 3;
+  const int w = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
+  if ((int)(blockIdx.x >> 3) >= each || w >= used) return;
+  int at = w * len;
+  const int end = min(at + len, total);
+  int b0 = 0, before = 0;                        // sequences b0 .. b0+63 at hand, places / HR before them
   while (at < end) {
-    int full = full_blocks(p, b0 + sg.lane);
-    int upto = before + wave_scan(full, sg.lane);
-    int all = __builtin_amdgcn_readlane(upto, 63);
+    int all = last_lane(upto);
     while (at >= all * HR) {                     // (ends: at < total)
       b0 += 64;
       before = all;
-      full = full_blocks(p, b0 + sg.lane);
-      upto = before + wave_scan(full, sg.lane);
-      all = __builtin_amdgcn_readlane(upto, 63);
+      places = unit_places(p, b0 + lane);
+      upto = before + wave_scan(places);
+      all = last_lane(upto);
     }
     const int in = __popcll(__ballot(at >= upto * HR));
-    full = __builtin_amdgcn_readlane(full, in);
-    const int x = at - (__builtin_amdgcn_readlane(upto, in) - full) * HR;
-    const int hr = x / full, t0 = x - hr * full;
-    const int t1 = min(full, t0 + end - at);
-    const int b = b0 + in, h = hr / p.n_rc, rc = hr - h * p.n_rc;
-    sg.begin(b, h, rc);
-    sg.blocks(b, h, t0, t1);
-    sg.end(rc, record_at(p, (int64_t)w + (int64_t)b * HR + hr));
+    const int mine = __builtin_amdgcn_readlane(places, in);
+    const int y = at - (__builtin_amdgcn_readlane(upto, in) - mine) * HR;
+    const int hr = (int)((uint32_t)y / (uint32_t)mine), t0 = y - hr * mine;
+    const int full = mine - kOpenTiles;
+    const int t1 = min(mine, t0 + end - at);
     at += t1 - t0;
+    if (t0 > full) continue;                     // (the rest of the places of open rows)
+    const int b = b0 + in, h = (int)((uint32_t)hr / (uint32_t)p.n_rc), rc = hr - h * p.n_rc;
+    sg.begin(b, h, rc);
+    sg.blocks(b, h, t0, min(t1, full));
+    if (t1 > full) sg.open_rows(b, h, rc, paged_len(p.kv_len[b], p.cols));
+    sg.end(rc, record_at(p, (int64_t)w + (int64_t)b * HR + hr));
   }
 }
 
 // ------------------------------------------------------------------------------ combine
-// One workgroup per output row: eight groups of 32 lanes take every eighth record, a lane four channels.
+// Groups of 32 lanes, a lane four channels.  SPLIT groups share an output row and take every SPLIT-th record each:
+// all eight of a workgroup where a unit has many records, or one group per row.
 constexpr int kCombineThreads = 256;
-constexpr int kCombineMax = 1024;      // records of a row: stretches of the line and its open rows
+constexpr int kCombineMax = 1024;      // records that a row can have: workgroups of the split
 
-__global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(PagedAttnKernelArgs p, int ks) {
-  __shared__ float s_w[kCombineMax + 1];
-  __shared__ float s_red[3][4];
-  __shared__ f32x4 s_o[8][32];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int row = blockIdx.x;                    // (b, kv head, row of its R)
-  const int R = p.R, HR = p.Hkv * p.n_rc;
-  const int bh = row / R, r = row - bh * R;
-  const int b = bh / p.Hkv, h = bh - b * p.Hkv;
-  const int rc = r / p.rpad, in = r - rc * p.rpad;
-  const int hr = h * p.n_rc + rc;
-  const int64_t unit = (int64_t)b * HR + hr;
-  // where the unit lies on the line
-  int sum = 0, mine = 0;
+template <int SPLIT>
+__global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(PagedAttnKernelArgs p) {
+  constexpr int kRows = 8 / SPLIT;               // output rows of a workgroup, all of one unit
+  constexpr int kAhead = 8;
+  __shared__ float s_m[8], s_l[8], s_v[8];
+  __shared__ f32x4 s_o[SPLIT > 1 ? 8 : 1][32];
+  const int tid = threadIdx.x, lane = tid & 63, g = tid >> 5, l32 = tid & 31;
+  const int HR = p.Hkv * p.n_rc;
+  const int per_unit = (p.rpad + kRows - 1) / kRows;
+  const int unit = (int)((uint32_t)blockIdx.x / (uint32_t)per_unit);
+  const int b = (int)((uint32_t)unit / (uint32_t)HR), hr = unit - b * HR;
+  const int h = (int)((uint32_t)hr / (uint32_t)p.n_rc), rc = hr - h * p.n_rc;
+  const int in = (blockIdx.x - unit * per_unit) * kRows + g / SPLIT, r = rc * p.rpad + in;
+  const bool row = in < p.rpad && r < p.R;
+  // where the unit lies on the line, and whose stretches it meets
+  int total = 0, before = 0, full = 0;
   for (int b0 = 0; b0 < p.B; b0 += 64) {
-    const int f = full_blocks(p, b0 + lane);
-    sum += f;
-    mine += b0 + lane < b ? f : 0;
+    const int f = unit_places(p, b0 + lane);
+    const int upto = wave_scan(f);
+    if (b >= b0 && b < b0 + 64) {
+      full = __builtin_amdgcn_readlane(f, b - b0);
+      before = total + __builtin_amdgcn_readlane(upto, b - b0) - full;
+      full -= kOpenTiles;
+    }
+    total += last_lane(upto);
   }
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) {
-    sum += __shfl_xor(sum, d, 64);
-    mine += __shfl_xor(mine, d, 64);
-  }
-  const int total = __builtin_amdgcn_readfirstlane(sum) * HR;
-  const int rounds = (total + p.n_wg * ks - 1) / (p.n_wg * ks);
-  const int per = (rounds > 0 ? rounds : 1) * ks;
-  const int full = full_blocks(p, b);
-  const int from = __builtin_amdgcn_readfirstlane(mine) * HR + hr * full;
-  const int w0 = from / per;
-  const int n = full > 0 ? (from + full - 1) / per - w0 + 1 : 0;      // records of blocks; one more of open rows
-  auto rec = [&](int k) { return record_at(p, k < n ? w0 + k + unit : (int64_t)p.n_wg + p.B * HR + unit); };
-  float mm = kNegBig;
-  for (int k = tid; k <= n; k += kCombineThreads) {
-    const float m = rec(k)[in];
-    s_w[k] = m;
-    mm = fmaxf(mm, m);
-  }
-  mm = wave_max(mm);
-  if (lane == 0) s_red[0][wave] = mm;
-  __syncthreads();
-  mm = fmaxf(fmaxf(s_red[0][0], s_red[0][1]), fmaxf(s_red[0][2], s_red[0][3]));
-  float l = 0.f, lv = 0.f;
-  for (int k = tid; k <= n; k += kCombineThreads) {
-    const float f = fast_exp2(s_w[k] - mm);
-    const float* x = rec(k);
-    l += x[p.rpad + in] * f;
-    lv += x[2 * p.rpad + in] * f;
-    s_w[k] = f;
-  }
-  l = wave_sum(l);
-  lv = wave_sum(lv);
-  if (lane == 0) {
-    s_red[1][wave] = l;
-    s_red[2][wave] = lv;
-  }
-  __syncthreads();
-  l = (s_red[1][0] + s_red[1][1]) + (s_red[1][2] + s_red[1][3]);
-  lv = (s_red[2][0] + s_red[2][1]) + (s_red[2][2] + s_red[2][3]);
-  const int g = tid >> 5, c4 = (tid & 31) * 4;
+  const int len = stretch_len(p, total * HR);
+  const int from = before * HR + hr * (full + kOpenTiles);
+  const int w0 = (int)((uint32_t)from / (uint32_t)len);
+  const int n = (int)((uint32_t)(from + full) / (uint32_t)len) - w0 + 1;
+  const float* rec = record_at(p, (int64_t)w0 + unit) + (row ? in : 0);
+  const int64_t step = (int64_t)p.rpad * 131;
+  // every group for itself: maximum, sums and output of its records, eight at a time
+  float mm = kNegBig, l = 0.f, lv = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int k = g; k <= n; k += 8)
-    o += *reinterpret_cast<const f32x4*>(rec(k) + 3 * p.rpad + in * 128 + c4) * s_w[k];
-  s_o[g][tid & 31] = o;
-  __syncthreads();
-  const int i = r / p.G, head = h * p.G + (r - i * p.G);
-  if (tid < 32) {
+  const float* orec = rec + 3 * p.rpad + (row ? in : 0) * 127 + l32 * 4;
+  for (int k0 = g % SPLIT; k0 < n; k0 += SPLIT * kAhead) {
+    f32x4 x[kAhead];
+    float m8[kAhead], l8[kAhead], v8[kAhead];
 #pragma unroll
-    for (int k = 1; k < 8; ++k) o += s_o[k][tid];
-    const float inv = 1.f / l;
-    uint2 y;
-    y.x = pack_bf16(o[0] * inv, o[1] * inv);
-    y.y = pack_bf16(o[2] * inv, o[3] * inv);
-    *reinterpret_cast<uint2*>(p.out + (int64_t)b * p.o_sb + (int64_t)i * p.o_sg + (int64_t)head * p.o_sh + c4) = y;
+    for (int k = 0; k < kAhead; ++k) {
+      const int at = k0 + SPLIT * k < n ? k0 + SPLIT * k : k0;
+      x[k] = *reinterpret_cast<const f32x4*>(orec + at * step);
+      m8[k] = rec[at * step];
+      l8[k] = rec[at * step + p.rpad];
+      v8[k] = rec[at * step + 2 * p.rpad];
+    }
+    float top = mm;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) top = fmaxf(top, m8[k]);
+    const float old = fast_exp2(mm - top);
+    mm = top;
+    o *= old;
+    l *= old;
+    lv *= old;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (k0 + SPLIT * k < n) {
+        const float f = fast_exp2(m8[k] - top);
+        o += x[k] * f;
+        l += l8[k] * f;
+        lv += v8[k] * f;
+      }
+    }
   }
-  if (tid == 0) {
+  if constexpr (SPLIT > 1) {
+    if (l32 == 0) {
+      s_m[g] = mm;
+      s_l[g] = l;
+      s_v[g] = lv;
+    }
+    s_o[g][l32] = o;
+    __syncthreads();
+    if (g % SPLIT != 0) return;
+    float top = mm;
+#pragma unroll
+    for (int k = 1; k < SPLIT; ++k) top = fmaxf(top, s_m[g + k]);
+    const float f = fast_exp2(mm - top);
+    o *= f;
+    l *= f;
+    lv *= f;
+#pragma unroll
+    for (int k = 1; k < SPLIT; ++k) {
+      const float f2 = fast_exp2(s_m[g + k] - top);
+      o += s_o[g + k][l32] * f2;
+      l += s_l[g + k] * f2;
+      lv += s_v[g + k] * f2;
+    }
+    mm = top;
+  }
+  if (!row) return;
+  const int i = r / p.G, head = h * p.G + (r - i * p.G);
+  const float inv = 1.f / l;
+  uint2 y;
+  y.x = pack_bf16(o[0] * inv, o[1] * inv);
+  y.y = pack_bf16(o[2] * inv, o[3] * inv);
+  *reinterpret_cast<uint2*>(p.out + (int64_t)b * p.o_sb + (int64_t)i * p.o_sg + (int64_t)head * p.o_sh + l32 * 4) = y;
+  if (l32 == 0) {
     const int64_t at = ((int64_t)b * p.Hq + head) * p.gamma + i;
     // ln(sum of exp) from base 2: ln 2 * (m + log2 l)
     if (p.lse != nullptr) p.lse[at] = 0.69314718055994531f * (mm + __log2f(l));
@@ -576,24 +616,28 @@ __global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(PagedAtt
 }
 
 template <int NB, int RG, int KS>
-hipError_t launch_shape(const PagedAttnKernelArgs& a, hipStream_t stream) {
+hipError_t launch_shape(PagedAttnKernelArgs a, hipStream_t stream) {
   static LdsLimitOnce limit;
   const void* fn = reinterpret_cast<const void*>(&paged_attn_kernel<NB, RG, KS>);
   constexpr size_t lds = Shape<NB, RG, KS>::kLds;
   hipError_t e = limit.ensure(fn, lds);
   if (e != hipSuccess) return e;
-  const int units = a.B * a.Hkv * a.n_rc;
-  paged_attn_kernel<NB, RG, KS><<<dim3((unsigned)(units + a.n_wg)), dim3(64 * RG * KS), lds, stream>>>(a);
+  a.streams = KS;
+  paged_attn_kernel<NB, RG, KS><<<dim3((unsigned)a.n_wg), dim3(64 * RG * KS), lds, stream>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  paged_combine_kernel<<<dim3((unsigned)(a.B * a.Hkv * a.R)), dim3(kCombineThreads), 0, stream>>>(a, KS);
+  const unsigned units = (unsigned)(a.B * a.Hkv * a.n_rc);
+  // records of a unit, about: n_wg / units + 1
+  if ((int64_t)units * 8 > a.n_wg)
+    paged_combine_kernel<1><<<dim3(units * (unsigned)((a.rpad + 7) / 8)), dim3(kCombineThreads), 0, stream>>>(a);
+  else
+    paged_combine_kernel<8><<<dim3(units * (unsigned)a.rpad), dim3(kCombineThreads), 0, stream>>>(a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-int paged_attn_workgroups(int rows, int num_cu) {
-  (void)rows;
+int paged_attn_workgroups(int num_cu) {
   const int n = 2 * num_cu / 8 * 8;
   return n < 8 ? 8 : n > kCombineMax ? kCombineMax : n;
 }
