@@ -288,6 +288,7 @@ struct PagedAttnKernelArgs {
   int B, gamma, Hq, Hkv;
   int G, R;                     // Hq / Hkv; query rows per kv head, ordered r = i * G + (h % G)
   int rpad, n_rc;               // rows per row chunk, row chunks
+  FastDiv div_g;                // by G
   int n_blocks, cols;
   int n_wg;                     // workgroups of the split kernel, a multiple of 8
   int streams;                  // waves of a workgroup with tiles of their own (set by the launch)

@@ -42,7 +42,7 @@ int plan_paged_attn(const lvspec_paged_attn_args* a, PagedPlan* pl) {
   if (a->Hq > 65536 || a->table_cols > LVSPEC_PAGED_MAX_BLOCKS) return LVSPEC_EUNSUPPORTED;
   pl->G = a->Hq / c.Hkv;
   pl->R = pl->G * a->gamma;
-  pl->n_rc = (pl->R + 63) / 64;
+  pl->n_rc = (pl->R + 31) / 32;
   pl->rpad = ((pl->R + pl->n_rc - 1) / pl->n_rc + 3) / 4 * 4;
   // tiles of the line, units and output rows are 32-bit numbers in the kernels
   const int64_t units = (int64_t)c.B * c.Hkv * pl->n_rc;   // (the open rows of a unit have eight places)
@@ -142,6 +142,7 @@ int lvspec_verify_attn_paged(const lvspec_paged_attn_args* a, void* stream) {
   k.k_tail = static_cast<const uint8_t*>(c.k_tail); k.v_tail = static_cast<const uint8_t*>(c.v_tail);
   k.table = a->table; k.kv_len = a->kv_len;
   k.B = c.B; k.gamma = a->gamma; k.Hq = a->Hq; k.Hkv = c.Hkv; k.G = pl.G; k.R = pl.R;
+  k.div_g = lvspec::make_fast_div((uint32_t)pl.G);
   k.rpad = pl.rpad; k.n_rc = pl.n_rc; k.n_blocks = c.n_blocks; k.cols = a->table_cols; k.n_wg = pl.n_wg;
   const float scale = a->scale > 0.f ? a->scale : 1.0f / __builtin_sqrtf((float)c.D);
   k.scale_log2e = scale * 1.4426950408889634f;

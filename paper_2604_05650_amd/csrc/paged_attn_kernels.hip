@@ -23,8 +23,9 @@ namespace lvspec {
 namespace {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kMergeStride = 132;      // floats per row in the merge buffer (pad)
+constexpr int kMergeStride = 132;      // floats per row in the merge buffer: output and two sums
 constexpr float kNegBig = -1.0e30f;
 constexpr int kBufferWord = 0x00020000;      // last word of a buffer resource: raw, 32-bit data
 
@@ -37,8 +38,8 @@ LVS_DEV u32x4 widen(uint32_t lo, uint32_t hi, float scale) {
 }
 
 // ------------------------------------------------------------------------------ the line of tiles
-// The units, sequence by sequence (HR = Hkv * n_rc each), lie one behind the other on a line: a unit's tiles of
-// 64 keys, then kOpenTiles places for its open rows, which take about as long as so many tiles.  The line is
+// The units, sequence by sequence (HR = Hkv * n_rc each), lie one behind the other on a line: a unit's
+// kOpenTiles places for its open rows, which take about as long as so many tiles, then its tiles.  The line is
 // cut into equal stretches, one per workgroup, short ones of whole rounds (a tile per stream); who has the first of the open
 // rows' places does them.  Every wave finds its place by itself.
 constexpr int kOpenTiles = 8;
@@ -67,13 +68,12 @@ LVS_DEV int stretch_len(const PagedAttnKernelArgs& p, int total) {
 }
 
 // ------------------------------------------------------------------------------ split
-// RG groups of NB * 16 rows by KS streams of tiles, a wave each.
-template <int NB, int RG, int KS>
+// NB blocks of 16 rows by KS streams of tiles, a wave each.
+template <int NB, int KS>
 struct Shape {
-  static constexpr int kWaves = RG * KS;
-  static constexpr int kRows = 16 * NB * RG;
-  static constexpr int kMergeBytes = (int)sizeof(float) * KS * kRows * (3 + kMergeStride);
-  static constexpr int kTurnBytes = kWaves * 32 * kRowBytes;      // values of 32 open rows per wave
+  static constexpr int kRows = 16 * NB;
+  static constexpr int kMergeBytes = (int)sizeof(float) * KS * kRows * (1 + kMergeStride);
+  static constexpr int kTurnBytes = KS * 32 * kRowBytes;      // values of 32 open rows per wave
   static constexpr int kLds = kMergeBytes > kTurnBytes ? kMergeBytes : kTurnBytes;
 };
 
@@ -146,20 +146,35 @@ LVS_DEV u32x4 pack8(const f32x4& a, const f32x4& b) {
   return u32x4{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3]), pack_bf16(b[0], b[1]), pack_bf16(b[2], b[3])};
 }
 
-template <int NB, int RG, int KS>
+// four channels of an output row; lane 0 of 32 its log-sum-exp and mass
+LVS_DEV void write_row(const PagedAttnKernelArgs& p, int b, int h, int r, int l32, const f32x4& o, float m, float l,
+                       float lv) {
+  const int i = (int)fast_div((uint32_t)r, p.div_g), head = h * p.G + (r - i * p.G);
+  const float inv = 1.f / l;
+  uint2 y;
+  y.x = pack_bf16(o[0] * inv, o[1] * inv);
+  y.y = pack_bf16(o[2] * inv, o[3] * inv);
+  *reinterpret_cast<uint2*>(p.out + (int64_t)b * p.o_sb + (int64_t)i * p.o_sg + (int64_t)head * p.o_sh + l32 * 4) = y;
+  if (l32 == 0) {
+    const int64_t at = ((int64_t)b * p.Hq + head) * p.gamma + i;
+    // ln(sum of exp) from base 2: ln 2 * (m + log2 l)
+    if (p.lse != nullptr) p.lse[at] = 0.69314718055994531f * (m + __log2f(l));
+    if (p.vis_mass != nullptr) p.vis_mass[at] = lv / l;
+  }
+}
+
+template <int NB, int KS, bool ONCE>
 struct Segment {
-  using W = Shape<NB, RG, KS>;
+  using W = Shape<NB, KS>;
   const PagedAttnKernelArgs& p;
   uint8_t* smem;
-  int wave, stream, rg;
+  int stream;
   u32x4 q[NB][4];          // channels 64 (c/2) + 16 g4 + 8 (c%2) .. +7 of row n16
   RowState<NB> st;
   int vis_b, vis_e;
 
   LVS_DEV Segment(const PagedAttnKernelArgs& a, uint8_t* lds) : p(a), smem(lds) {
-    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    stream = wave % KS;
-    rg = wave / KS;
+    stream = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   }
 
   // The lane's number, row or token (n16) and quarter (g4).  Every part of a segment takes them anew: what
@@ -179,32 +194,31 @@ struct Segment {
     const int n16 = me.n16, g4 = me.g4;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      const int in = (rg * NB + nb) * 16 + n16, r = rc * p.rpad + in;
-      const bool valid = in < p.rpad && r < p.R;
-      const int rcl = r < p.R ? r : p.R - 1;
-      const int qi = rcl / p.G;
+      const int r = rc * p.rpad + nb * 16 + n16;
+      const int rcl = r < p.R ? r : p.R - 1;     // (rows past the last one: that row again, to no output)
+      const int qi = (int)fast_div((uint32_t)rcl, p.div_g);
       const uint16_t* qp = p.q + (int64_t)b * p.q_sb + (int64_t)qi * p.q_sg +
                            (int64_t)(h * p.G + (rcl - qi * p.G)) * p.q_sh;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(qp + 64 * (c >> 1) + 16 * g4 + 8 * (c & 1));
-        q[nb][c] = valid ? x : u32x4{0u, 0u, 0u, 0u};
-      }
+      for (int c = 0; c < 4; ++c)
+        q[nb][c] = *reinterpret_cast<const u32x4*>(qp + 64 * (c >> 1) + 16 * g4 + 8 * (c & 1));
 #pragma unroll
       for (int db = 0; db < 8; ++db) st.acc[nb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
       st.m[nb] = kNegBig;
       st.l[nb] = st.lv[nb] = 0.f;
     }
-    vis_b = p.vis_begin != nullptr ? p.vis_begin[b] : 0;
-    vis_e = p.vis_begin != nullptr ? p.vis_end[b] : 0;
+    vis_b = vis_e = 0;
+    if (p.vis_begin != nullptr) {
+      vis_b = __builtin_amdgcn_readfirstlane(p.vis_begin[b]);
+      vis_e = __builtin_amdgcn_readfirstlane(p.vis_end[b]);
+    }
   }
 
   // tiles t0 .. t1-1 of a unit
   LVS_DEV void blocks(int b, int h, int t0, int t1) {
     const Lane me;
     const int lane = me.lane, n16 = me.n16, g4 = me.g4;
-    // (tiles that several waves read stay in the caches)
-    constexpr int kPolicy = RG == 1 ? kCopyStream : kCopyDefault;
+    constexpr int kPolicy = ONCE ? kCopyStream : kCopyDefault;
     const int mine = (t1 - t0 - stream + KS - 1) / KS;
     if (mine <= 0) return;
     const int32_t* row = p.table + (int64_t)b * p.cols;
@@ -239,15 +253,23 @@ struct Segment {
       for (int x = 0; x < 8; ++x)
         v[x] = __builtin_amdgcn_raw_buffer_load_b128(from, v_at + (x & 3) * 1024, (x >> 2) * 4096, kPolicy);
     };
+    // (in this order: the loop waits for what it needs next and for nothing behind it)
     fetch(0);
+    __builtin_amdgcn_sched_barrier(0);
     int id = __builtin_amdgcn_readlane(ids, 0);
     load_k(id);
+    __builtin_amdgcn_sched_barrier(0);
     load_v(id);
+    __builtin_amdgcn_sched_barrier(0);
     const float c = p.scale_log2e;
     for (int j = 0; j < mine; ++j) {
       const float k_scale = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, k_scales), j & 63));
       const float v_scale = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v_scales), j & 63));
-      if (((j + 1) & 63) == 0) fetch(j + 1);
+      if (((j + 1) & 63) == 0) {
+        fetch(j + 1);
+        // (waited for here, once in 64 tiles: the loop's own waits then go by the tiles alone)
+        asm volatile("" : "+v"(ids), "+v"(k_scales), "+v"(v_scales));
+      }
       const int next = j + 1 < mine ? __builtin_amdgcn_readlane(ids, (j + 1) & 63) : -1;
       f32x4 s[NB][4];
 #pragma unroll
@@ -288,28 +310,45 @@ struct Segment {
     }
   }
 
+  // Makes values that are not finite zero; bit r: row r of the 32 has some.
+  LVS_DEV uint32_t take_out(u32x4 (&v)[8]) {
+    uint32_t rows = 0;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      bool bad = false;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool lo = (v[x][i] & 0x7f80u) == 0x7f80u, hi = (v[x][i] & 0x7f800000u) == 0x7f800000u;
+        bad |= lo || hi;
+        v[x][i] = (lo ? 0u : v[x][i] & 0xffffu) | (hi ? 0u : v[x][i] & 0xffff0000u);
+      }
+      const unsigned long long at = __ballot(bad);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) rows |= ((at >> (16 * i)) & 0xffffull) != 0ull ? 1u << (4 * x + i) : 0u;
+    }
+    return rows;
+  }
+
   // open rows: positions L / 64 * 64 .. L + gamma - 1, in pieces of 32 keys, one stream each
-  LVS_DEV void open_rows(int b, int h, int rc, int L) {
+  LVS_DEV void open_rows(int b, int h, int rc, int L, bool again) {
     const Lane me;
     const int n16 = me.n16, g4 = me.g4;
     const int base = L & ~(kPageTokens - 1);
     const int n = L - base + p.gamma;
-    uint32_t rowmask[NB];
+    uint32_t rowmask[NB];            // draft rows that row n16 sees
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      const int in = (rg * NB + nb) * 16 + n16, r = rc * p.rpad + in;
-      const int draft_row = in < p.rpad && r < p.R ? r / p.G : -1;
-      rowmask[nb] = 0u;
-#pragma unroll
-      for (int j = 0; j < 32; ++j) rowmask[nb] = draft_row == j ? p.draft_mask[j] : rowmask[nb];
-      rowmask[nb] &= 0xffffffffu >> (32 - p.gamma);
+      const int r = rc * p.rpad + nb * 16 + n16;
+      rowmask[nb] = p.draft_mask[fast_div((uint32_t)(r < p.R ? r : p.R - 1), p.div_g)] & (0xffffffffu >> (32 - p.gamma));
     }
     const int64_t unit = ((int64_t)b * p.Hkv + h) * (kTailRows * kRowBytes);
     const uint8_t* kt = p.k_tail + unit;
     const uint8_t* vt = p.v_tail + unit;
-    const uint32_t turn = lds_addr(smem) + wave * (32 * kRowBytes);
+    const uint32_t turn = lds_addr(smem) + stream * (32 * kRowBytes);
     const float c = p.scale_log2e;
-    for (int piece = stream; piece * 32 < n; piece += KS) {
+    if (again) __syncthreads();      // (the segment before this one has been read from LDS)
+    // (from the last stream on: the first ones have the odd tiles)
+    for (int piece = KS - 1 - stream; piece * 32 < n; piece += KS) {
       const int p0 = base + piece * 32;
       u32x4 k[2][4], v[8];
 #pragma unroll
@@ -324,22 +363,16 @@ struct Segment {
       // Rows behind the last draft are nobody's: zero.  A value that is not finite would reach rows that do
       // not see its key, as 0 * inf: it is zero here as well, and its rows are remembered for below.
       uint32_t odd = 0;
+      u16x2 top = {0, 0};
 #pragma unroll
       for (int x = 0; x < 8; ++x) {
-        const bool there = p0 + 4 * x + g4 < L + p.gamma;
-        bool bad = false;
+        v[x] = p0 + 4 * x + g4 < L + p.gamma ? v[x] : u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) bad |= (v[x][i] & 0x7f80u) == 0x7f80u || (v[x][i] & 0x7f800000u) == 0x7f800000u;
-        const unsigned long long at = __ballot(there && bad);
-        if (at != 0ull) {
+        for (int i = 0; i < 4; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, v[x][i] & 0x7fff7fffu));
+      }
+      if (__any(top[0] >= 0x7f80 || top[1] >= 0x7f80)) odd = take_out(v);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            odd |= ((at >> (16 * i)) & 0xffffull) != 0ull ? 1u << (4 * x + i) : 0u;
-            v[x][i] = (v[x][i] & 0x7f80u) == 0x7f80u ? v[x][i] & 0xffff0000u : v[x][i];
-            v[x][i] = (v[x][i] & 0x7f800000u) == 0x7f800000u ? v[x][i] & 0xffffu : v[x][i];
-          }
-        }
-        v[x] = there ? v[x] : u32x4{0u, 0u, 0u, 0u};
+      for (int x = 0; x < 8; ++x) {
         const int r = 4 * x + g4;
         *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(turn + r * kRowBytes +
                                                                ((n16 ^ rows32_swz(r & 15)) << 4)) = v[x];
@@ -352,13 +385,12 @@ struct Segment {
           f32x4 z = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int x = 0; x < 4; ++x) z = mfma16(k[kb][x], q[nb][x], z);
+          // bit k: row n16 sees key k of the piece; committed keys first, then the draft rows
+          const int old = L - p0;
+          const uint32_t sees = old >= 32 ? 0xffffffffu
+                                : old >= 0 ? ((1u << old) - 1u) | (rowmask[nb] << old) : rowmask[nb] >> min(-old, 31);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int j = p0 + 16 * kb + 4 * g4 + i - L;       // draft row of the key
-            const int jc = j < 0 ? 0 : j > 31 ? 31 : j;
-            const bool sees = j < 0 || (j < 32 && ((rowmask[nb] >> jc) & 1u) != 0u);
-            z[i] = sees ? z[i] : -INFINITY;
-          }
+          for (int i = 0; i < 4; ++i) z[i] = (sees >> (4 * g4)) & (1u << (16 * kb + i)) ? z[i] : -INFINITY;
           s[nb][kb] = z;
         }
       softmax_tile<NB, 2>(st, s, c);
@@ -400,71 +432,102 @@ struct Segment {
     }
   }
 
-  // the streams' states into one record
-  LVS_DEV void end(int rc, float* rec) {
+  // streams that have something of a segment of n tiles, and of the open rows or not
+  LVS_DEV uint32_t active(int n, bool open, int L) {
+    uint32_t on = n >= KS ? (1u << KS) - 1u : (1u << max(n, 0)) - 1u;
+    if (open) {
+      const int pieces = ((L & (kPageTokens - 1)) + p.gamma + 31) >> 5;      // at most 3
+      on |= ((1u << KS) - 1u) & ~((1u << max(KS - pieces, 0)) - 1u);
+    }
+    return on;
+  }
+
+  // The active streams' states to LDS, each brought to the row's common maximum first, so that what is left is
+  // sums: [KS][kRows] maxima, then per stream and row 132 floats, the output, the denominator and its share
+  // on the video span.
+  LVS_DEV void gather(uint32_t on) {
     const Lane me;
     const int n16 = me.n16, g4 = me.g4;
-    float* sm_m = reinterpret_cast<float*>(smem);          // [KS][kRows]
-    float* sm_l = sm_m + KS * W::kRows;
-    float* sm_v = sm_l + KS * W::kRows;
-    float* sm_o = sm_v + KS * W::kRows;                    // [KS][kRows][kMergeStride]
+    float* sm_m = reinterpret_cast<float*>(smem);
     __syncthreads();
+    if (g4 == 0) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) sm_m[stream * W::kRows + nb * 16 + n16] = st.m[nb];
+    }
+    __syncthreads();
+    if (((on >> stream) & 1u) == 0u) return;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      float l = st.l[nb], lv = st.lv[nb];
+      const int row = nb * 16 + n16;
+      float mm = sm_m[row];
+#pragma unroll
+      for (int k = 1; k < KS; ++k) mm = fmaxf(mm, sm_m[k * W::kRows + row]);
+      const float f = fast_exp2(st.m[nb] - mm);
+      float* o = sm_m + KS * W::kRows + (stream * W::kRows + row) * kMergeStride;
+#pragma unroll
+      for (int db = 0; db < 8; ++db) *reinterpret_cast<f32x4*>(o + 16 * db + 4 * g4) = st.acc[nb][db] * f;
+      float l = st.l[nb] * f, lv = st.lv[nb] * f;
       l += xor_shuffle(l, 16);
       l += xor_shuffle(l, 32);
       lv += xor_shuffle(lv, 16);
       lv += xor_shuffle(lv, 32);
-      const int r = stream * W::kRows + (rg * NB + nb) * 16 + n16;
-      if (g4 == 0) {
-        sm_m[r] = st.m[nb];
-        sm_l[r] = l;
-        sm_v[r] = lv;
-      }
-#pragma unroll
-      for (int db = 0; db < 8; ++db)
-        *reinterpret_cast<f32x4*>(sm_o + (size_t)r * kMergeStride + 16 * db + 4 * g4) = st.acc[nb][db];
+      if (g4 == 0) *reinterpret_cast<float2*>(o + 128) = float2{l, lv};
     }
+  }
+
+  // sums over the active streams of four floats of a row
+  LVS_DEV f32x4 merged(uint32_t on, int row, int c4) {
+    const float* o = reinterpret_cast<const float*>(smem) + KS * W::kRows + row * kMergeStride + c4;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+      if ((on >> k) & 1u) sum += *reinterpret_cast<const f32x4*>(o + k * W::kRows * kMergeStride);
+    return sum;
+  }
+  LVS_DEV float merged_max(int row) {
+    const float* sm_m = reinterpret_cast<const float*>(smem);
+    float mm = sm_m[row];
+#pragma unroll
+    for (int k = 1; k < KS; ++k) mm = fmaxf(mm, sm_m[k * W::kRows + row]);
+    return mm;
+  }
+
+  // the merged state into a record
+  LVS_DEV void end(uint32_t on, int rc, float* rec) {
+    gather(on);
     __syncthreads();
-    int rows = p.R - rc * p.rpad;
-    rows = rows < p.rpad ? rows : p.rpad;
-    for (int row = threadIdx.x; row < rows; row += 64 * W::kWaves) {
-      float mm = sm_m[row];
-#pragma unroll
-      for (int k = 1; k < KS; ++k) mm = fmaxf(mm, sm_m[k * W::kRows + row]);
-      float l = 0.f, lv = 0.f;
-#pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        const float f = fast_exp2(sm_m[k * W::kRows + row] - mm);
-        l += sm_l[k * W::kRows + row] * f;
-        lv += sm_v[k * W::kRows + row] * f;
-      }
-      rec[row] = mm;
-      rec[p.rpad + row] = l;
-      rec[2 * p.rpad + row] = lv;
+    const int rows = min(p.R - rc * p.rpad, p.rpad);
+    for (int idx = threadIdx.x; idx < rows * 32; idx += 64 * KS) {
+      const int row = idx >> 5, l32 = idx & 31;
+      *reinterpret_cast<f32x4*>(rec + 3 * p.rpad + row * 128 + l32 * 4) = merged(on, row, l32 * 4);
     }
-    for (int idx = threadIdx.x; idx < rows * 32; idx += 64 * W::kWaves) {
-      const int row = idx >> 5, c4 = (idx & 31) * 4;
-      float mm = sm_m[row];
-#pragma unroll
-      for (int k = 1; k < KS; ++k) mm = fmaxf(mm, sm_m[k * W::kRows + row]);
-      f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int k = 0; k < KS; ++k)
-        o += *reinterpret_cast<const f32x4*>(sm_o + (size_t)(k * W::kRows + row) * kMergeStride + c4) *
-             fast_exp2(sm_m[k * W::kRows + row] - mm);
-      *reinterpret_cast<f32x4*>(rec + 3 * p.rpad + row * 128 + c4) = o;
+    for (int row = threadIdx.x; row < rows; row += 64 * KS) {
+      const f32x4 l = merged(on, row, 128);
+      rec[row] = merged_max(row);
+      rec[p.rpad + row] = l[0];
+      rec[2 * p.rpad + row] = l[1];
+    }
+  }
+
+  // the merged state of a whole unit into the outputs
+  LVS_DEV void finish(uint32_t on, int b, int h, int rc) {
+    gather(on);
+    __syncthreads();
+    const int rows = min(p.R - rc * p.rpad, p.rpad);
+    for (int idx = threadIdx.x; idx < rows * 32; idx += 64 * KS) {
+      const int row = idx >> 5, l32 = idx & 31;
+      const f32x4 l = merged(on, row, 128);
+      write_row(p, b, h, rc * p.rpad + row, l32, merged(on, row, l32 * 4), merged_max(row), l[0], l[1]);
     }
   }
 };
 
 LVS_DEV float* record_at(const PagedAttnKernelArgs& p, int64_t i) { return p.ws + i * ((int64_t)p.rpad * 131); }
 
-template <int NB, int RG, int KS>
-__global__ __launch_bounds__(64 * RG * KS, 2) void paged_attn_kernel(PagedAttnKernelArgs p) {
+template <int NB, int KS, bool ONCE>
+__global__ __launch_bounds__(64 * KS, 2) void paged_attn_kernel(PagedAttnKernelArgs p) {
   extern __shared__ __align__(256) uint8_t smem[];
-  Segment<NB, RG, KS> sg(p, smem);
+  Segment<NB, KS, ONCE> sg(p, smem);
   const int HR = p.Hkv * p.n_rc, lane = threadIdx.x & 63;
   int places = unit_places(p, lane);
   int upto = wave_scan(places), total = last_lane(upto);
@@ -491,22 +554,37 @@ __global__ __launch_bounds__(64 * RG * KS, 2) void paged_attn_kernel(PagedAttnKe
     const int in = __popcll(__ballot(at >= upto * HR));
     const int mine = __builtin_amdgcn_readlane(places, in);
     const int y = at - (__builtin_amdgcn_readlane(upto, in) - mine) * HR;
-    const int hr = (int)((uint32_t)y / (uint32_t)mine), t0 = y - hr * mine;
-    const int full = mine - kOpenTiles;
-    const int t1 = min(mine, t0 + end - at);
-    at += t1 - t0;
-    if (t0 > full) continue;                     // (the rest of the places of open rows)
+    const int hr = (int)((uint32_t)y / (uint32_t)mine), p0 = y - hr * mine;
+    const int p1 = min(mine, p0 + end - at);
+    at += p1 - p0;
+    if (p0 > 0 && p1 <= kOpenTiles) continue;    // (only places of open rows, not the first)
     const int b = b0 + in, h = (int)((uint32_t)hr / (uint32_t)p.n_rc), rc = hr - h * p.n_rc;
+    const int L = paged_len(p.kv_len[b], p.cols), t0 = max(p0 - kOpenTiles, 0), t1 = p1 - kOpenTiles;
     sg.begin(b, h, rc);
-    sg.blocks(b, h, t0, min(t1, full));
-    if (t1 > full) sg.open_rows(b, h, rc, paged_len(p.kv_len[b], p.cols));
-    sg.end(rc, record_at(p, (int64_t)w + (int64_t)b * HR + hr));
+    if (p0 == 0) sg.open_rows(b, h, rc, L, true);
+    sg.blocks(b, h, t0, t1);
+    sg.end(sg.active(t1 - t0, p0 == 0, L), rc, record_at(p, (int64_t)w + (int64_t)b * HR + hr));
   }
+}
+
+// One workgroup per unit, straight to the output: for tables so narrow that cutting a unit does not pay.
+template <int NB, int KS, bool ONCE>
+__global__ __launch_bounds__(64 * KS, 2) void paged_attn_unit_kernel(PagedAttnKernelArgs p) {
+  extern __shared__ __align__(256) uint8_t smem[];
+  Segment<NB, KS, ONCE> sg(p, smem);
+  const int bh = (int)((uint32_t)blockIdx.x / (uint32_t)p.n_rc), rc = blockIdx.x - bh * p.n_rc;
+  const int b = (int)((uint32_t)bh / (uint32_t)p.Hkv), h = bh - b * p.Hkv;
+  const int L = paged_len(p.kv_len[b], p.cols);
+  sg.begin(b, h, rc);
+  sg.blocks(b, h, 0, L >> kPageShift);
+  sg.open_rows(b, h, rc, L, false);
+  sg.finish(sg.active(L >> kPageShift, true, L), b, h, rc);
 }
 
 // ------------------------------------------------------------------------------ combine
 // Groups of 32 lanes, a lane four channels.  SPLIT groups share an output row and take every SPLIT-th record each:
 // all eight of a workgroup where a unit has many records, or one group per row.
+constexpr int kUnitTiles = 16;         // columns of a table up to which a unit is one workgroup's
 constexpr int kCombineThreads = 256;
 constexpr int kCombineMax = 1024;      // records that a row can have: workgroups of the split
 
@@ -538,10 +616,13 @@ __global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(PagedAtt
   }
   const int len = stretch_len(p, total * HR);
   const int from = before * HR + hr * (full + kOpenTiles);
-  const int w0 = (int)((uint32_t)from / (uint32_t)len);
-  const int n = (int)((uint32_t)(from + full) / (uint32_t)len) - w0 + 1;
-  const float* rec = record_at(p, (int64_t)w0 + unit) + (row ? in : 0);
+  // (the stretch of the first place, and those from the first tile's to the last one's)
+  const int first = (int)((uint32_t)from / (uint32_t)len);
+  const int next = full > 0 ? max((int)((uint32_t)(from + kOpenTiles) / (uint32_t)len), first + 1) : first + 1;
+  const int n = full > 0 ? max((int)((uint32_t)(from + kOpenTiles + full - 1) / (uint32_t)len) - next + 2, 1) : 1;
   const int64_t step = (int64_t)p.rpad * 131;
+  const float* rec = record_at(p, (int64_t)first + unit) + (row ? in : 0);
+  const int64_t skip = (next - first - 1) * step;        // between the first record and the others
   // every group for itself: maximum, sums and output of its records, eight at a time
   float mm = kNegBig, l = 0.f, lv = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -552,10 +633,11 @@ __global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(PagedAtt
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       const int at = k0 + SPLIT * k < n ? k0 + SPLIT * k : k0;
-      x[k] = *reinterpret_cast<const f32x4*>(orec + at * step);
-      m8[k] = rec[at * step];
-      l8[k] = rec[at * step + p.rpad];
-      v8[k] = rec[at * step + 2 * p.rpad];
+      const int64_t off = at * step + (at > 0 ? skip : 0);
+      x[k] = *reinterpret_cast<const f32x4*>(orec + off);
+      m8[k] = rec[off];
+      l8[k] = rec[off + p.rpad];
+      v8[k] = rec[off + 2 * p.rpad];
     }
     float top = mm;
 #pragma unroll
@@ -600,30 +682,17 @@ __global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(PagedAtt
     }
     mm = top;
   }
-  if (!row) return;
-  const int i = r / p.G, head = h * p.G + (r - i * p.G);
-  const float inv = 1.f / l;
-  uint2 y;
-  y.x = pack_bf16(o[0] * inv, o[1] * inv);
-  y.y = pack_bf16(o[2] * inv, o[3] * inv);
-  *reinterpret_cast<uint2*>(p.out + (int64_t)b * p.o_sb + (int64_t)i * p.o_sg + (int64_t)head * p.o_sh + l32 * 4) = y;
-  if (l32 == 0) {
-    const int64_t at = ((int64_t)b * p.Hq + head) * p.gamma + i;
-    // ln(sum of exp) from base 2: ln 2 * (m + log2 l)
-    if (p.lse != nullptr) p.lse[at] = 0.69314718055994531f * (mm + __log2f(l));
-    if (p.vis_mass != nullptr) p.vis_mass[at] = lv / l;
-  }
+  if (row) write_row(p, b, h, r, l32, o, mm, l, lv);
 }
 
-template <int NB, int RG, int KS>
-hipError_t launch_shape(PagedAttnKernelArgs a, hipStream_t stream) {
+template <int NB, int KS, bool ONCE>
+hipError_t launch_line(PagedAttnKernelArgs a, hipStream_t stream) {
   static LdsLimitOnce limit;
-  const void* fn = reinterpret_cast<const void*>(&paged_attn_kernel<NB, RG, KS>);
-  constexpr size_t lds = Shape<NB, RG, KS>::kLds;
-  hipError_t e = limit.ensure(fn, lds);
+  constexpr size_t lds = Shape<NB, KS>::kLds;
+  hipError_t e = limit.ensure(reinterpret_cast<const void*>(&paged_attn_kernel<NB, KS, ONCE>), lds);
   if (e != hipSuccess) return e;
   a.streams = KS;
-  paged_attn_kernel<NB, RG, KS><<<dim3((unsigned)a.n_wg), dim3(64 * RG * KS), lds, stream>>>(a);
+  paged_attn_kernel<NB, KS, ONCE><<<dim3((unsigned)a.n_wg), dim3(64 * KS), lds, stream>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   const unsigned units = (unsigned)(a.B * a.Hkv * a.n_rc);
@@ -635,6 +704,17 @@ hipError_t launch_shape(PagedAttnKernelArgs a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+template <int NB, int KS, bool ONCE>
+hipError_t launch_units(const PagedAttnKernelArgs& a, hipStream_t stream) {
+  static LdsLimitOnce limit;
+  constexpr size_t lds = Shape<NB, KS>::kLds;
+  hipError_t e = limit.ensure(reinterpret_cast<const void*>(&paged_attn_unit_kernel<NB, KS, ONCE>), lds);
+  if (e != hipSuccess) return e;
+  const unsigned units = (unsigned)(a.B * a.Hkv * a.n_rc);
+  paged_attn_unit_kernel<NB, KS, ONCE><<<dim3(units), dim3(64 * KS), lds, stream>>>(a);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 int paged_attn_workgroups(int num_cu) {
@@ -643,9 +723,13 @@ int paged_attn_workgroups(int num_cu) {
 }
 
 hipError_t launch_paged_attn(const PagedAttnKernelArgs& a, hipStream_t stream) {
-  if (a.rpad <= 16) return launch_shape<1, 1, 4>(a, stream);
-  if (a.rpad <= 32) return launch_shape<2, 1, 4>(a, stream);
-  return launch_shape<2, 2, 2>(a, stream);
+  const bool once = a.n_rc == 1;
+  if (a.cols <= kUnitTiles) {
+    if (a.rpad <= 16) return once ? launch_units<1, 8, true>(a, stream) : launch_units<1, 8, false>(a, stream);
+    return once ? launch_units<2, 8, true>(a, stream) : launch_units<2, 8, false>(a, stream);
+  }
+  if (a.rpad <= 16) return once ? launch_line<1, 4, true>(a, stream) : launch_line<1, 4, false>(a, stream);
+  return once ? launch_line<2, 4, true>(a, stream) : launch_line<2, 4, false>(a, stream);
 }
 
 }  // namespace lvspec

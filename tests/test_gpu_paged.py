@@ -251,12 +251,13 @@ ATTNS = [
 ]
 
 
+@pytest.mark.parametrize("spare_cols", [1, 50])        # a unit in one workgroup, or all of them on a line
 @pytest.mark.parametrize("i", range(len(ATTNS)))
-def test_attention(L, i):
+def test_attention(L, i, spare_cols):
     c = ATTNS[i]
     kv, g, Hq, Hkv = c["kv"], c["g"], c.get("Hq", 4), c.get("Hkv", 2)
     B = len(kv)
-    cache, table = ready(L, 50 + i, B, Hkv, kv)
+    cache, table = ready(L, 50 + i, B, Hkv, kv, spare_cols=spare_cols)
     q = normal(200 + i, (B, g, Hq, D))
     mask = tree(c["branches"], g // c["branches"]) if "branches" in c else None
     vis = ([5] * B, [max(5, n * 2 // 3) for n in kv]) if i % 2 else None
@@ -275,10 +276,11 @@ def test_attention_strides_and_span(L):
     check_attention(L, q, cache, table, kv, ([13, -5, 0], [333, 64, 1]))
 
 
-def test_attention_reads_declared_rows_only(L):
+@pytest.mark.parametrize("spare_cols", [3, 50])
+def test_attention_reads_declared_rows_only(L, spare_cols):
     """Unused blocks, table entries behind the length and ring rows of nobody hold NaN."""
     kv, g = [200, 64, 30, 0], 5
-    cache, table = ready(L, 92, 4, 2, kv, extra=4, spare_cols=3)
+    cache, table = ready(L, 92, 4, 2, kv, extra=4, spare_cols=spare_cols)
     q = normal(93, (4, g, 8, D))
     want = check_attention(L, q, cache, table, kv).clone()
     used = {int(table[b, j]) for b in range(4) for j in range(kv[b] // T)}
@@ -299,11 +301,12 @@ def test_attention_reads_declared_rows_only(L):
     assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("spare_cols", [1, 50])
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
-def test_attention_masked_draft_rows_do_not_reach_others(L, value):
+def test_attention_masked_draft_rows_do_not_reach_others(L, value, spare_cols):
     """A draft row that is not finite changes the rows that see it and no other."""
     kv, g = [100, 64], 6
-    cache, table = ready(L, 94, 2, 2, kv)
+    cache, table = ready(L, 94, 2, 2, kv, spare_cols=spare_cols)
     q = normal(95, (2, g, 8, D))
     want = L.verify_attn_paged(q, cache, i32(table), i32(kv)).clone()
     for b, n in enumerate(kv):
