@@ -27,7 +27,7 @@ typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kMergeStride = 132;      // floats per row in the merge buffer: output and two sums
 constexpr float kNegBig = -1.0e30f;
-constexpr int kBufferWord = 0x00020000;      // last word of a buffer resource: raw, 32-bit data
+constexpr uint32_t kBufferWord = 0x00020000;      // last word of a buffer resource: raw, 32-bit data
 
 // eight e4m3 times 2^e as bf16 (exact)
 LVS_DEV u32x4 widen(uint32_t lo, uint32_t hi, float scale) {
@@ -35,6 +35,44 @@ LVS_DEV u32x4 widen(uint32_t lo, uint32_t hi, float scale) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x, scale, decltype(upper)::value));
   };
   return u32x4{two(lo, std::false_type{}), two(lo, std::true_type{}), two(hi, std::false_type{}), two(hi, std::true_type{})};
+}
+
+// ------------------------------------------------------------------------------ tiles to LDS
+// A wave's ring: one slot of keys, one of values.  Sixteen lanes of an operand read hold sixteen tokens (or
+// channels) and would ask memory for sixteen rows at a time, a cache line each; copies go row by row instead,
+// and LDS has the 16-byte chunks of a row in an order in which the operand reads meet no bank twice: with
+// the four passes of 16 lanes of such a read (lds_load16), chunk c of token t at c ^ (t>>1 & 1 | t>>4 << 1), chunk c
+// of channel d at c ^ v_place(d >> 2).
+constexpr int kRingBytes = 2 * kPageBytes;
+
+LVS_DEV int v_place(int q) { return ((q >> 1) & 1) | (((q ^ (q >> 1)) & 1) << 1); }    // 0 2 3 1
+
+// Eight copies of 1 KiB of a block of the pool to a slot, lane l of copy y from offset y * 1024 + o[y / 2].  No
+// block: a buffer of no bytes, nothing is fetched and zeros are written.  (The compiler does not know them as
+// LDS writes or loads: waits are wait_copies, and m0 is as before.)
+template <bool ONCE>
+LVS_DEV void copy_page(const uint8_t* pool, int id, int64_t head, uint32_t slot, int o0, int o1, int o2, int o3,
+                       int n_heads) {
+  const uint64_t at = (uint64_t)(pool + ((int64_t)max(id, 0) * n_heads + head) * kPageBytes);
+  const u32x4 from = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, id >= 0 ? (uint32_t)kPageBytes : 0u, kBufferWord};
+  const uint32_t to = __builtin_amdgcn_readfirstlane(slot);
+  uint32_t keep, far;
+#define LVS_COPY_1(O, POLICY) "buffer_load_dwordx4 " O ", %7, %1 offen" POLICY " lds\n\t"
+#define LVS_COPY_NEXT "s_add_u32 m0, m0, 0x400\n\ts_add_u32 %1, %1, 0x400\n\ts_nop 0\n\t"
+#define LVS_COPY(P)                                                                                   \
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %6\n\ts_mov_b32 %1, 0\n\ts_nop 0\n\t"                 \
+               LVS_COPY_1("%2", P) LVS_COPY_NEXT LVS_COPY_1("%2", P) LVS_COPY_NEXT                    \
+               LVS_COPY_1("%3", P) LVS_COPY_NEXT LVS_COPY_1("%3", P) LVS_COPY_NEXT                    \
+               LVS_COPY_1("%4", P) LVS_COPY_NEXT LVS_COPY_1("%4", P) LVS_COPY_NEXT                    \
+               LVS_COPY_1("%5", P) LVS_COPY_NEXT LVS_COPY_1("%5", P) "s_mov_b32 m0, %0"               \
+               : "=&s"(keep), "=&s"(far) : "v"(o0), "v"(o1), "v"(o2), "v"(o3), "s"(to), "s"(from) : "memory", "scc")
+  if constexpr (ONCE)
+    LVS_COPY(" nt");
+  else
+    LVS_COPY("");
+#undef LVS_COPY
+#undef LVS_COPY_NEXT
+#undef LVS_COPY_1
 }
 
 // ------------------------------------------------------------------------------ the line of tiles
@@ -73,8 +111,7 @@ template <int NB, int KS>
 struct Shape {
   static constexpr int kRows = 16 * NB;
   static constexpr int kMergeBytes = (int)sizeof(float) * KS * kRows * (1 + kMergeStride);
-  static constexpr int kTurnBytes = KS * 32 * kRowBytes;      // values of 32 open rows per wave
-  static constexpr int kLds = kMergeBytes > kTurnBytes ? kMergeBytes : kTurnBytes;
+  static constexpr int kLds = kMergeBytes > KS * kRingBytes ? kMergeBytes : KS * kRingBytes;
 };
 
 template <int NB>
@@ -83,9 +120,12 @@ struct RowState {
   float m[NB], l[NB], lv[NB];
 };
 
-// scores of NK blocks of 16 keys to probabilities (in place); the running maximum and the sums follow
+// Scores of NK blocks of 16 keys to probabilities (in place); the running maximum and the sums follow.
+// `first`: there is nothing to rescale yet.  The maximum is exact: a reference that is taken anew only for
+// scores 2^8 above it saves 1 to 4 % of the time and costs the exact 1 of the largest probability (error
+// against 64 bits 2.2e-3 -> 2.5e-3).
 template <int NB, int NK>
-LVS_DEV void softmax_tile(RowState<NB>& st, f32x4 (&s)[NB][NK], float c) {
+LVS_DEV void softmax_tile(RowState<NB>& st, f32x4 (&s)[NB][NK], float c, bool first) {
   bool grow = false;
   float top[NB];
 #pragma unroll
@@ -104,10 +144,12 @@ LVS_DEV void softmax_tile(RowState<NB>& st, f32x4 (&s)[NB][NK], float c) {
       const float x = max_rows(max_halves(fmaxf(st.m[nb], top[nb])));
       const float alpha = fast_exp2(st.m[nb] - x);
       st.m[nb] = x;
-      st.l[nb] *= alpha;
-      st.lv[nb] *= alpha;
+      if (!first) {
+        st.l[nb] *= alpha;
+        st.lv[nb] *= alpha;
 #pragma unroll
-      for (int db = 0; db < 8; ++db) st.acc[nb][db] *= alpha;
+        for (int db = 0; db < 8; ++db) st.acc[nb][db] *= alpha;
+      }
     }
   }
 #pragma unroll
@@ -172,6 +214,7 @@ struct Segment {
   u32x4 q[NB][4];          // channels 64 (c/2) + 16 g4 + 8 (c%2) .. +7 of row n16
   RowState<NB> st;
   int vis_b, vis_e;
+  bool fresh;              // nothing in the state yet
 
   LVS_DEV Segment(const PagedAttnKernelArgs& a, uint8_t* lds) : p(a), smem(lds) {
     stream = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -207,6 +250,7 @@ struct Segment {
       st.m[nb] = kNegBig;
       st.l[nb] = st.lv[nb] = 0.f;
     }
+    fresh = true;
     vis_b = vis_e = 0;
     if (p.vis_begin != nullptr) {
       vis_b = __builtin_amdgcn_readfirstlane(p.vis_begin[b]);
@@ -216,61 +260,57 @@ struct Segment {
 
   // tiles t0 .. t1-1 of a unit
   LVS_DEV void blocks(int b, int h, int t0, int t1) {
-    const Lane me;
-    const int lane = me.lane, n16 = me.n16, g4 = me.g4;
-    constexpr int kPolicy = ONCE ? kCopyStream : kCopyDefault;
     const int mine = (t1 - t0 - stream + KS - 1) / KS;
     if (mine <= 0) return;
+    const Lane me;
+    const int lane = me.lane, n16 = me.n16, g4 = me.g4;
     const int32_t* row = p.table + (int64_t)b * p.cols;
-    const int k_at = (16 * (n16 >> 2) + (n16 & 3)) * 128 + 16 * g4;           // token, channel
-    const int v_at = n16 * kPageTokens + 16 * g4;                              // channel, token
-    // blocks and scales of 64 tiles, one per lane.  An entry that names no block of the pool is -1.
+    // blocks of 64 tiles, one per lane.  An entry that names no block of the pool is -1.
     int ids;
-    float k_scales, v_scales;
     auto fetch = [&](int j0) {
       const int t = t0 + stream + KS * (j0 + lane);
       ids = t < t1 ? row[t] : -1;
       ids = (uint32_t)ids < (uint32_t)p.n_blocks ? ids : -1;
-      const int64_t at = (int64_t)max(ids, 0) * p.Hkv + h;
-      k_scales = p.k_scale[at];
-      v_scales = p.v_scale[at];
+      asm volatile("" : "+v"(ids));      // (waited for here: the loop has no loads but its copies)
     };
-    // (no block: a buffer of no bytes, whose loads fetch nothing and give zero)
-    auto buffer = [&](const uint8_t* pool, int id) {
-      const int64_t at = ((int64_t)max(id, 0) * p.Hkv + h) * kPageBytes;
-      return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(pool + at), 0, id >= 0 ? kPageBytes : 0, kBufferWord);
+    // scales by scalar loads, which do not count among the copies
+    auto scale_of = [&](const float* scale, int id) {
+      return *(const __attribute__((address_space(4))) float*)(uintptr_t)(scale + ((int64_t)max(id, 0) * p.Hkv + h));
     };
-    u32x4 k[8], v[8];
-    auto load_k = [&](int id) {          // block x / 2 of 16 keys, channels 64 (x%2) ..
-      const auto from = buffer(p.k8, id);
+    const uint32_t k_slot = lds_addr(smem) + stream * kRingBytes, v_slot = k_slot + kPageBytes;
+    // global side of the copies: row and chunk that belong at lane's place (see k_place, v_place)
+    const int k_from = (lane >> 3) * 128, k_chunk = (lane & 7) ^ ((lane >> 4) & 1);
+    int k_off[4];
 #pragma unroll
-      for (int x = 0; x < 8; ++x)
-        k[x] = __builtin_amdgcn_raw_buffer_load_b128(from, k_at + (x >> 1) * 512 + (x & 1) * 64, 0, kPolicy);
-    };
-    auto load_v = [&](int id) {          // channels 16 x ..
-      const auto from = buffer(p.v8, id);
-#pragma unroll
-      for (int x = 0; x < 8; ++x)
-        v[x] = __builtin_amdgcn_raw_buffer_load_b128(from, v_at + (x & 3) * 1024, (x >> 2) * 4096, kPolicy);
-    };
-    // (in this order: the loop waits for what it needs next and for nothing behind it)
+    for (int y = 0; y < 4; ++y) k_off[y] = k_from + ((k_chunk ^ (y << 1)) << 4);
+    const int v_off = (lane >> 2) * kPageTokens + (((lane & 3) ^ v_place(lane >> 4)) << 4);
+    auto copy_k = [&](int id) { copy_page<ONCE>(p.k8, id, h, k_slot, k_off[0], k_off[1], k_off[2], k_off[3], p.Hkv); };
+    auto copy_v = [&](int id) { copy_page<ONCE>(p.v8, id, h, v_slot, v_off, v_off, v_off, v_off, p.Hkv); };
+    // LDS side of the operands: token 16 (n16/4) + 4 kb + n16%4, chunk 4 half + g4; channel 16 x + n16, chunk g4
+    const uint32_t k_at = k_slot + (16 * (n16 >> 2) + (n16 & 3)) * 128;
+    const int k_key = ((n16 >> 1) & 1) | ((n16 >> 2) << 1);
+    const uint32_t k_at0 = k_at + ((g4 ^ k_key) << 4), k_at1 = k_at + (((4 + g4) ^ k_key) << 4);
+    const uint32_t v_at = v_slot + n16 * kPageTokens + ((g4 ^ v_place(n16 >> 2)) << 4);
     fetch(0);
-    __builtin_amdgcn_sched_barrier(0);
     int id = __builtin_amdgcn_readlane(ids, 0);
-    load_k(id);
-    __builtin_amdgcn_sched_barrier(0);
-    load_v(id);
-    __builtin_amdgcn_sched_barrier(0);
+    copy_k(id);
+    copy_v(id);
+    float k_scale = scale_of(p.k_scale, id), v_scale = scale_of(p.v_scale, id);
     const float c = p.scale_log2e;
     for (int j = 0; j < mine; ++j) {
-      const float k_scale = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, k_scales), j & 63));
-      const float v_scale = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v_scales), j & 63));
-      if (((j + 1) & 63) == 0) {
-        fetch(j + 1);
-        // (waited for here, once in 64 tiles: the loop's own waits then go by the tiles alone)
-        asm volatile("" : "+v"(ids), "+v"(k_scales), "+v"(v_scales));
+      const bool more = j + 1 < mine;
+      if (((j + 1) & 63) == 0) fetch(j + 1);
+      const int next = more ? __builtin_amdgcn_readlane(ids, (j + 1) & 63) : -1;
+      u32x4 k[8];
+      wait_copies<8>();                // all but V's
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb) {
+        k[2 * kb] = lds_load16(k_at0 + kb * 512);
+        k[2 * kb + 1] = lds_load16(k_at1 + kb * 512);
       }
-      const int next = j + 1 < mine ? __builtin_amdgcn_readlane(ids, (j + 1) & 63) : -1;
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (more) copy_k(next);
+      const float k_next = scale_of(p.k_scale, next), v_next = scale_of(p.v_scale, next);
       f32x4 s[NB][4];
 #pragma unroll
       for (int kb = 0; kb < 4; ++kb) {
@@ -284,18 +324,29 @@ struct Segment {
           for (int nb = 0; nb < NB; ++nb) s[nb][kb] = mfma16(a, q[nb][x], s[nb][kb]);
         }
       }
-      load_k(next);
+      u32x4 pr[NB][2];
       if (id >= 0) {
-        softmax_tile<NB, 4>(st, s, c);
+        softmax_tile<NB, 4>(st, s, c, fresh);
+        fresh = false;
         const int key0 = (t0 + stream + KS * j) * kPageTokens;
         span_mass<NB, 4>(st, s, key0, kPageTokens, vis_b, vis_e,
                          [&](int kb, int i) { return key0 + 16 * g4 + 4 * kb + i; });
-        u32x4 pr[NB][2];
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
           pr[nb][0] = pack8(s[nb][0], s[nb][1]);
           pr[nb][1] = pack8(s[nb][2], s[nb][3]);
         }
+      }
+      u32x4 v[8];
+      if (more)
+        wait_copies<8>();              // all but the next K's
+      else
+        wait_copies<0>();
+#pragma unroll
+      for (int x = 0; x < 8; ++x) v[x] = lds_load16(v_at + x * 1024);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (more) copy_v(next);
+      if (id >= 0) {
 #pragma unroll
         for (int db = 0; db < 8; ++db)
 #pragma unroll
@@ -305,8 +356,9 @@ struct Segment {
             for (int nb = 0; nb < NB; ++nb) st.acc[nb][db] = mfma16(a, pr[nb][y], st.acc[nb][db]);
           }
       }
-      load_v(next);
       id = next;
+      k_scale = k_next;
+      v_scale = v_next;
     }
   }
 
@@ -330,7 +382,7 @@ struct Segment {
   }
 
   // open rows: positions L / 64 * 64 .. L + gamma - 1, in pieces of 32 keys, one stream each
-  LVS_DEV void open_rows(int b, int h, int rc, int L, bool again) {
+  LVS_DEV void open_rows(int b, int h, int rc, int L) {
     const Lane me;
     const int n16 = me.n16, g4 = me.g4;
     const int base = L & ~(kPageTokens - 1);
@@ -344,9 +396,8 @@ struct Segment {
     const int64_t unit = ((int64_t)b * p.Hkv + h) * (kTailRows * kRowBytes);
     const uint8_t* kt = p.k_tail + unit;
     const uint8_t* vt = p.v_tail + unit;
-    const uint32_t turn = lds_addr(smem) + stream * (32 * kRowBytes);
+    const uint32_t turn = lds_addr(smem) + stream * kRingBytes;
     const float c = p.scale_log2e;
-    if (again) __syncthreads();      // (the segment before this one has been read from LDS)
     // (from the last stream on: the first ones have the odd tiles)
     for (int piece = KS - 1 - stream; piece * 32 < n; piece += KS) {
       const int p0 = base + piece * 32;
@@ -393,7 +444,8 @@ struct Segment {
           for (int i = 0; i < 4; ++i) z[i] = (sees >> (4 * g4)) & (1u << (16 * kb + i)) ? z[i] : -INFINITY;
           s[nb][kb] = z;
         }
-      softmax_tile<NB, 2>(st, s, c);
+      softmax_tile<NB, 2>(st, s, c, fresh);
+      fresh = false;
       span_mass<NB, 2>(st, s, p0, 32, vis_b, vis_e, [&](int kb, int i) { return p0 + 16 * kb + 4 * g4 + i; });
       u32x4 pr[NB];
 #pragma unroll
@@ -541,6 +593,7 @@ __global__ __launch_bounds__(64 * KS, 2) void paged_attn_kernel(PagedAttnKernelA
   if ((int)(blockIdx.x >> 3) >= each || w >= used) return;
   int at = w * len;
   const int end = min(at + len, total);
+  bool again = false;
   int b0 = 0, before = 0;                        // sequences b0 .. b0+63 at hand, places / HR before them
   while (at < end) {
     int all = last_lane(upto);
@@ -560,8 +613,10 @@ __global__ __launch_bounds__(64 * KS, 2) void paged_attn_kernel(PagedAttnKernelA
     if (p0 > 0 && p1 <= kOpenTiles) continue;    // (only places of open rows, not the first)
     const int b = b0 + in, h = (int)((uint32_t)hr / (uint32_t)p.n_rc), rc = hr - h * p.n_rc;
     const int L = paged_len(p.kv_len[b], p.cols), t0 = max(p0 - kOpenTiles, 0), t1 = p1 - kOpenTiles;
+    if (again) __syncthreads();                  // (the segment before this one has been read from LDS)
+    again = true;
     sg.begin(b, h, rc);
-    if (p0 == 0) sg.open_rows(b, h, rc, L, true);
+    if (p0 == 0) sg.open_rows(b, h, rc, L);
     sg.blocks(b, h, t0, t1);
     sg.end(sg.active(t1 - t0, p0 == 0, L), rc, record_at(p, (int64_t)w + (int64_t)b * HR + hr));
   }
@@ -577,7 +632,7 @@ __global__ __launch_bounds__(64 * KS, 2) void paged_attn_unit_kernel(PagedAttnKe
   const int L = paged_len(p.kv_len[b], p.cols);
   sg.begin(b, h, rc);
   sg.blocks(b, h, 0, L >> kPageShift);
-  sg.open_rows(b, h, rc, L, false);
+  sg.open_rows(b, h, rc, L);
   sg.finish(sg.active(L >> kPageShift, true, L), b, h, rc);
 }
 
