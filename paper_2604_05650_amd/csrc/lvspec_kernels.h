@@ -290,8 +290,7 @@ struct PagedAttnKernelArgs {
   int rpad, n_rc;               // rows per row chunk, row chunks
   FastDiv div_g;                // by G
   int n_blocks, cols;
-  int n_wg;                     // workgroups of the split kernel, a multiple of 8
-  int streams;                  // waves of a workgroup with tiles of their own (set by the launch)
+  int n_wg, wg_shift;           // workgroups that the chip holds at once, 2^wg_shift >= 8
   float scale_log2e;
   const int32_t* vis_begin;     // nullptr = no span
   const int32_t* vis_end;
@@ -303,6 +302,6 @@ struct PagedAttnKernelArgs {
   uint32_t draft_mask[32];
 };
 hipError_t launch_paged_attn(const PagedAttnKernelArgs& a, hipStream_t stream);
-int paged_attn_workgroups(int num_cu);   // n_wg
+int paged_attn_workgroups(int num_cu);   // n_wg: two per CU, rounded down to a power of two
 
 }  // namespace lvspec

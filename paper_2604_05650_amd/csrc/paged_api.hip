@@ -144,6 +144,7 @@ int lvspec_verify_attn_paged(const lvspec_paged_attn_args* a, void* stream) {
   k.B = c.B; k.gamma = a->gamma; k.Hq = a->Hq; k.Hkv = c.Hkv; k.G = pl.G; k.R = pl.R;
   k.div_g = lvspec::make_fast_div((uint32_t)pl.G);
   k.rpad = pl.rpad; k.n_rc = pl.n_rc; k.n_blocks = c.n_blocks; k.cols = a->table_cols; k.n_wg = pl.n_wg;
+  k.wg_shift = __builtin_ctz((unsigned)pl.n_wg);
   const float scale = a->scale > 0.f ? a->scale : 1.0f / __builtin_sqrtf((float)c.D);
   k.scale_log2e = scale * 1.4426950408889634f;
   k.vis_begin = a->vis_begin; k.vis_end = a->vis_end;

@@ -54,7 +54,9 @@ template <bool ONCE>
 LVS_DEV void copy_page(const uint8_t* pool, int id, int64_t head, uint32_t slot, int o0, int o1, int o2, int o3,
                        int n_heads) {
   const uint64_t at = (uint64_t)(pool + ((int64_t)max(id, 0) * n_heads + head) * kPageBytes);
-  const u32x4 from = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, id >= 0 ? (uint32_t)kPageBytes : 0u, kBufferWord};
+  u32x4 from = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, id >= 0 ? (uint32_t)kPageBytes : 0u, kBufferWord};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) from[i] = __builtin_amdgcn_readfirstlane(from[i]);      // (in scalar registers)
   const uint32_t to = __builtin_amdgcn_readfirstlane(slot);
   uint32_t keep, far;
 #define LVS_COPY_1(O, POLICY) "buffer_load_dwordx4 " O ", %7, %1 offen" POLICY " lds\n\t"
@@ -76,12 +78,17 @@ LVS_DEV void copy_page(const uint8_t* pool, int id, int64_t head, uint32_t slot,
 }
 
 // ------------------------------------------------------------------------------ the line of tiles
-// The units, sequence by sequence (HR = Hkv * n_rc each), lie one behind the other on a line: a unit's
-// kOpenTiles places for its open rows, which take about as long as so many tiles, then its tiles.  The line is
-// cut into equal stretches, one per workgroup, short ones of whole rounds (a tile per stream); who has the first of the open
-// rows' places does them.  Every wave finds its place by itself.
+// A unit (sequence, kv head, row chunk) has kOpenTiles places for its open rows, which take about as long as
+// so many tiles, and a place per tile of 64 keys.  Two ways to divide them:
+//   the line: all units one behind the other, sequence by sequence (HR = Hkv * n_rc units each), cut into
+//     equal stretches, one per workgroup.  Nobody waits for anybody, but a stretch over the end of a unit is two
+//     segments, and a segment has 5 us of its own (first loads, merge);
+//   parts: every unit in equal parts of at most so many places that there are no more parts than workgroups.
+// The line is taken where a stretch is long (kLineLeast).  Who has the first of a unit's places does its open rows.
+// Every wave finds its place by itself.
 constexpr int kOpenTiles = 8;
-constexpr int kWholeRounds = 32;
+constexpr int kLineLeast = 32;
+constexpr int kPartRounds = 5;
 
 LVS_DEV int wave_scan(int x) {               // inclusive sum over the lanes
   auto add = [&](uint32_t y) { x += (int)y; };
@@ -97,12 +104,60 @@ LVS_DEV int last_lane(int x) { return __builtin_amdgcn_readlane(x, 63); }
 
 LVS_DEV int full_blocks(const PagedAttnKernelArgs& p, int b) { return paged_len(p.kv_len[b], p.cols) >> kPageShift; }
 
-// places of a sequence's unit on the line
-LVS_DEV int unit_places(const PagedAttnKernelArgs& p, int b) { return b < p.B ? full_blocks(p, b) + kOpenTiles : 0; }
+struct Cut {
+  int total;           // places of all units (line), or parts of all units
+  int len;             // places of a stretch; 0: parts
+  uint32_t inv;        // parts: about 2^32 / most places of a part
+  // a sequence's share of the line, or the parts of one of its units
+  LVS_DEV int share(int places) const { return places == 0 || len > 0 ? places : 1 + (int)__umulhi((uint32_t)(places - 1), inv); }
+};
 
-LVS_DEV int stretch_len(const PagedAttnKernelArgs& p, int total) {
-  const int each = (int)((uint32_t)(total + p.n_wg - 1) / (uint32_t)p.n_wg);
-  return each >= kWholeRounds ? each : (each + p.streams - 1) / p.streams * p.streams;
+// Exact, but some thirty instructions one behind the other, a tenth of a microsecond; and about.
+LVS_DEV int divide(int x, int d) { return (int)((uint32_t)x / (uint32_t)d); }
+LVS_DEV int about(int x, int d) { return (int)((float)x * __builtin_amdgcn_rcpf((float)d)); }
+
+// places of the units of sequences b0 .. b0+63, one per lane; 0 behind the last one
+LVS_DEV int places_of(const PagedAttnKernelArgs& p, int b) { return b < p.B ? full_blocks(p, b) + kOpenTiles : 0; }
+
+// places0: those of the first 64 sequences
+template <int KS>
+LVS_DEV Cut cut_units(const PagedAttnKernelArgs& p, int lane, int places0) {
+  int sum = last_lane(wave_scan(places0)), most = (int)wave_max_u32((uint32_t)places0);
+  for (int b0 = 64; b0 < p.B; b0 += 64) {
+    const int x = places_of(p, b0 + lane);
+    sum += last_lane(wave_scan(x));
+    most = max(most, (int)wave_max_u32((uint32_t)x));
+  }
+  const int HR = p.Hkv * p.n_rc, units = p.B * HR, cus = p.n_wg >> 1;
+  Cut c;
+  const int total = sum * HR, stretch = (total + p.n_wg - 1) >> p.wg_shift;
+  c.total = total;
+  c.len = stretch;
+  if (stretch >= kLineLeast) return c;
+  // Parts for one workgroup per CU (and some more of open rows only), or, where those take many rounds of
+  // the streams, for two.
+  c.len = 0;
+  int limit = max(cus, units) + min(units, cus >> 3), part = 0;
+  for (int wide = 0; wide < 2; ++wide) {
+    part = max((about(total, limit) + KS - 1) / KS * KS, kOpenTiles);
+    while (true) {
+      c.inv = (uint32_t)(4294967040.f * __builtin_amdgcn_rcpf((float)part));
+      int n = last_lane(wave_scan(c.share(places0)));
+      for (int b0 = 64; b0 < p.B; b0 += 64) n += last_lane(wave_scan(c.share(places_of(p, b0 + lane))));
+      c.total = n * HR;
+      if (c.total <= limit || part >= most) break;
+      part += max(part >> 3, KS) / KS * KS;
+    }
+    if (part <= kPartRounds * KS || limit >= p.n_wg) break;
+    limit = p.n_wg;
+  }
+  // lengths so unequal that the longest part is well above the average
+  const int even = about(total, limit);
+  if (stretch >= kLineLeast / 2 && min(part, most) > even + (even >> 1) + kOpenTiles) {
+    c.total = total;
+    c.len = stretch;
+  }
+  return c;
 }
 
 // ------------------------------------------------------------------------------ split
@@ -581,44 +636,54 @@ __global__ __launch_bounds__(64 * KS, 2) void paged_attn_kernel(PagedAttnKernelA
   extern __shared__ __align__(256) uint8_t smem[];
   Segment<NB, KS, ONCE> sg(p, smem);
   const int HR = p.Hkv * p.n_rc, lane = threadIdx.x & 63;
-  int places = unit_places(p, lane);
-  int upto = wave_scan(places), total = last_lane(upto);
-  for (int b0 = 64; b0 < p.B; b0 += 64) total += last_lane(wave_scan(unit_places(p, b0 + lane)));
-  total *= HR;
-  const int len = stretch_len(p, total);
-  const int used = (int)((uint32_t)(total + len - 1) / (uint32_t)len);     // stretches, at most n_wg
-  // stretches that follow each other go to one XCD, which has the records of a unit in its L2
+  const int places0 = places_of(p, lane);
+  const Cut cut = cut_units<KS>(p, lane, places0);
+  const int len = max(cut.len, 1);
+  const int used = cut.len > 0 ? divide(cut.total + len - 1, len) : cut.total;       // workgroups with work
+  // work that follows each other goes to one XCD, which has the records of a unit in its L2
   const int each = (used + 7) >> 3;
   const int w = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
   if ((int)(blockIdx.x >> 3) >= each || w >= used) return;
   int at = w * len;
-  const int end = min(at + len, total);
+  const int end = min(at + len, cut.total);
   bool again = false;
-  int b0 = 0, before = 0;                        // sequences b0 .. b0+63 at hand, places / HR before them
+  int b0 = 0, before = 0;                        // sequences b0 .. b0+63 at hand, shares before them
+  int places = places0, upto = wave_scan(cut.share(places));
   while (at < end) {
     int all = last_lane(upto);
     while (at >= all * HR) {                     // (ends: at < total)
       b0 += 64;
       before = all;
-      places = unit_places(p, b0 + lane);
-      upto = before + wave_scan(places);
+      places = places_of(p, b0 + lane);
+      upto = before + wave_scan(cut.share(places));
       all = last_lane(upto);
     }
     const int in = __popcll(__ballot(at >= upto * HR));
-    const int mine = __builtin_amdgcn_readlane(places, in);
+    const int unit_places = __builtin_amdgcn_readlane(places, in);
+    const int mine = cut.share(unit_places);
     const int y = at - (__builtin_amdgcn_readlane(upto, in) - mine) * HR;
-    const int hr = (int)((uint32_t)y / (uint32_t)mine), p0 = y - hr * mine;
-    const int p1 = min(mine, p0 + end - at);
+    const int hr = divide(y, mine), x = y - hr * mine;
+    const int b = b0 + in, h = ONCE ? hr : divide(hr, p.n_rc), rc = hr - h * p.n_rc;
+    int p0 = x, p1 = min(mine, x + end - at);    // places of the unit
     at += p1 - p0;
+    if (cut.len == 0) {
+      const int q = divide(unit_places, mine), r = unit_places - q * mine;      // the first r have one more
+      p0 = x * q + min(x, r);
+      p1 = p0 + q + (x < r ? 1 : 0);
+    }
     if (p0 > 0 && p1 <= kOpenTiles) continue;    // (only places of open rows, not the first)
-    const int b = b0 + in, h = (int)((uint32_t)hr / (uint32_t)p.n_rc), rc = hr - h * p.n_rc;
-    const int L = paged_len(p.kv_len[b], p.cols), t0 = max(p0 - kOpenTiles, 0), t1 = p1 - kOpenTiles;
+    const int t0 = max(p0 - kOpenTiles, 0), t1 = p1 - kOpenTiles;
     if (again) __syncthreads();                  // (the segment before this one has been read from LDS)
     again = true;
+    const int L = p0 == 0 ? paged_len(p.kv_len[b], p.cols) : 0;      // (for the open rows)
     sg.begin(b, h, rc);
     if (p0 == 0) sg.open_rows(b, h, rc, L);
     sg.blocks(b, h, t0, t1);
-    sg.end(sg.active(t1 - t0, p0 == 0, L), rc, record_at(p, (int64_t)w + (int64_t)b * HR + hr));
+    const uint32_t on = sg.active(t1 - t0, p0 == 0, L);
+    if (cut.len == 0 && mine == 1)
+      sg.finish(on, b, h, rc);
+    else
+      sg.end(on, rc, record_at(p, cut.len > 0 ? (int64_t)w + (int64_t)b * HR + hr : w));
   }
 }
 
@@ -639,11 +704,9 @@ __global__ __launch_bounds__(64 * KS, 2) void paged_attn_unit_kernel(PagedAttnKe
 // ------------------------------------------------------------------------------ combine
 // Groups of 32 lanes, a lane four channels.  SPLIT groups share an output row and take every SPLIT-th record each:
 // all eight of a workgroup where a unit has many records, or one group per row.
-constexpr int kUnitTiles = 16;         // columns of a table up to which a unit is one workgroup's
 constexpr int kCombineThreads = 256;
-constexpr int kCombineMax = 1024;      // records that a row can have: workgroups of the split
 
-template <int SPLIT>
+template <int SPLIT, int KS>
 __global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(PagedAttnKernelArgs p) {
   constexpr int kRows = 8 / SPLIT;               // output rows of a workgroup, all of one unit
   constexpr int kAhead = 8;
@@ -657,27 +720,35 @@ __global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(PagedAtt
   const int h = (int)((uint32_t)hr / (uint32_t)p.n_rc), rc = hr - h * p.n_rc;
   const int in = (blockIdx.x - unit * per_unit) * kRows + g / SPLIT, r = rc * p.rpad + in;
   const bool row = in < p.rpad && r < p.R;
-  // where the unit lies on the line, and whose stretches it meets
-  int total = 0, before = 0, full = 0;
-  for (int b0 = 0; b0 < p.B; b0 += 64) {
-    const int f = unit_places(p, b0 + lane);
+  // where the unit lies, and whose records are its own
+  int places = places_of(p, lane);
+  const Cut cut = cut_units<KS>(p, lane, places);
+  int before = 0, share = 0;
+  for (int b0 = 0; b0 <= b; b0 += 64) {
+    if (b0 > 0) places = places_of(p, b0 + lane);
+    const int f = cut.share(places);
     const int upto = wave_scan(f);
-    if (b >= b0 && b < b0 + 64) {
-      full = __builtin_amdgcn_readlane(f, b - b0);
-      before = total + __builtin_amdgcn_readlane(upto, b - b0) - full;
-      full -= kOpenTiles;
+    if (b < b0 + 64) {
+      share = __builtin_amdgcn_readlane(f, b - b0);
+      before += __builtin_amdgcn_readlane(upto, b - b0) - share;
+    } else {
+      before += last_lane(upto);
     }
-    total += last_lane(upto);
   }
-  const int len = stretch_len(p, total * HR);
-  const int from = before * HR + hr * (full + kOpenTiles);
-  // (the stretch of the first place, and those from the first tile's to the last one's)
-  const int first = (int)((uint32_t)from / (uint32_t)len);
-  const int next = full > 0 ? max((int)((uint32_t)(from + kOpenTiles) / (uint32_t)len), first + 1) : first + 1;
-  const int n = full > 0 ? max((int)((uint32_t)(from + kOpenTiles + full - 1) / (uint32_t)len) - next + 2, 1) : 1;
+  if (cut.len == 0 && share == 1) return;        // (one part: it has written the output)
+  const int from = before * HR + hr * share;
   const int64_t step = (int64_t)p.rpad * 131;
-  const float* rec = record_at(p, (int64_t)first + unit) + (row ? in : 0);
-  const int64_t skip = (next - first - 1) * step;        // between the first record and the others
+  int64_t at0 = from, skip = 0;                  // first record, and records between it and the others
+  int n = share;
+  if (cut.len > 0) {
+    // the stretch of the first place, and those from the first tile's to the last one's
+    const int first = divide(from, cut.len), full = share - kOpenTiles;
+    const int next = full > 0 ? max(divide(from + kOpenTiles, cut.len), first + 1) : first + 1;
+    n = full > 0 ? max(divide(from + share - 1, cut.len) - next + 2, 1) : 1;
+    at0 = (int64_t)first + unit;
+    skip = (next - first - 1) * step;
+  }
+  const float* rec = record_at(p, at0) + (row ? in : 0);
   // every group for itself: maximum, sums and output of its records, eight at a time
   float mm = kNegBig, l = 0.f, lv = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -740,22 +811,30 @@ __global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(PagedAtt
   if (row) write_row(p, b, h, r, l32, o, mm, l, lv);
 }
 
+// Columns of a table up to which every unit is one workgroup's.  The longest sequence may have as many blocks, so the
+// more units there are, the more of them pay: they fill the chip anyway.
+int64_t unit_columns(int64_t units, int64_t cus) {
+  if (units >= 2 * cus) return (int64_t)1 << 30;
+  return units >= cus ? 64 : units >= cus / 4 ? 32 : 20;
+}
+
 template <int NB, int KS, bool ONCE>
-hipError_t launch_line(PagedAttnKernelArgs a, hipStream_t stream) {
+hipError_t launch_line(const PagedAttnKernelArgs& a, hipStream_t stream) {
   static LdsLimitOnce limit;
   constexpr size_t lds = Shape<NB, KS>::kLds;
   hipError_t e = limit.ensure(reinterpret_cast<const void*>(&paged_attn_kernel<NB, KS, ONCE>), lds);
   if (e != hipSuccess) return e;
-  a.streams = KS;
-  paged_attn_kernel<NB, KS, ONCE><<<dim3((unsigned)a.n_wg), dim3(64 * KS), lds, stream>>>(a);
+  const unsigned units = (unsigned)(a.B * a.Hkv * a.n_rc);
+  // (a part for every unit at least; the grid is a multiple of 8)
+  const unsigned wgs = ((units > (unsigned)a.n_wg ? units : (unsigned)a.n_wg) + 7) / 8 * 8;
+  paged_attn_kernel<NB, KS, ONCE><<<dim3(wgs), dim3(64 * KS), lds, stream>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const unsigned units = (unsigned)(a.B * a.Hkv * a.n_rc);
   // records of a unit, about: n_wg / units + 1
   if ((int64_t)units * 8 > a.n_wg)
-    paged_combine_kernel<1><<<dim3(units * (unsigned)((a.rpad + 7) / 8)), dim3(kCombineThreads), 0, stream>>>(a);
+    paged_combine_kernel<1, KS><<<dim3(units * (unsigned)((a.rpad + 7) / 8)), dim3(kCombineThreads), 0, stream>>>(a);
   else
-    paged_combine_kernel<8><<<dim3(units * (unsigned)a.rpad), dim3(kCombineThreads), 0, stream>>>(a);
+    paged_combine_kernel<8, KS><<<dim3(units * (unsigned)a.rpad), dim3(kCombineThreads), 0, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -773,13 +852,15 @@ hipError_t launch_units(const PagedAttnKernelArgs& a, hipStream_t stream) {
 }  // namespace
 
 int paged_attn_workgroups(int num_cu) {
-  const int n = 2 * num_cu / 8 * 8;
-  return n < 8 ? 8 : n > kCombineMax ? kCombineMax : n;
+  int n = 8;
+  while (2 * n <= 2 * num_cu && n < 1024) n *= 2;
+  return n;
 }
 
 hipError_t launch_paged_attn(const PagedAttnKernelArgs& a, hipStream_t stream) {
   const bool once = a.n_rc == 1;
-  if (a.cols <= kUnitTiles) {
+  const int64_t units = (int64_t)a.B * a.Hkv * a.n_rc, cus = a.n_wg / 2;
+  if (a.cols <= unit_columns(units, cus)) {
     if (a.rpad <= 16) return once ? launch_units<1, 8, true>(a, stream) : launch_units<1, 8, false>(a, stream);
     return once ? launch_units<2, 8, true>(a, stream) : launch_units<2, 8, false>(a, stream);
   }
