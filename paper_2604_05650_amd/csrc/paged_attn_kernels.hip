@@ -38,36 +38,35 @@ LVS_DEV u32x4 widen(uint32_t lo, uint32_t hi, float scale) {
 }
 
 // ------------------------------------------------------------------------------ tiles to LDS
-// A wave's ring: one slot of keys, one of values.  Sixteen lanes of an operand read hold sixteen tokens (or
-// channels) and would ask memory for sixteen rows at a time, a cache line each; copies go row by row instead,
-// and LDS has the 16-byte chunks of a row in an order in which the operand reads meet no bank twice: with
-// the four passes of 16 lanes of such a read (lds_load16), chunk c of token t at c ^ (t>>1 & 1 | t>>4 << 1), chunk c
-// of channel d at c ^ v_place(d >> 2).
+// A wave's ring: one slot of keys, one of values.  An operand read has as many tokens (or channels) as lanes and
+// would ask memory for as many rows at a time, a cache line each; copies go row by row instead, and LDS has the
+// 16-byte chunks of a row in an order in which the operand reads meet no bank twice: chunk c of token t at
+// c ^ k_place(t), chunk c of channel d at c ^ v_place(d / 4), functions of the core (Rows16, Rows32).
 constexpr int kRingBytes = 2 * kPageBytes;
 
-LVS_DEV int v_place(int q) { return ((q >> 1) & 1) | (((q ^ (q >> 1)) & 1) << 1); }    // 0 2 3 1
-
-// Eight copies of 1 KiB of a block of the pool to a slot, lane l of copy y from offset y * 1024 + o[y / 2].  No
-// block: a buffer of no bytes, nothing is fetched and zeros are written.  (The compiler does not know them as
-// LDS writes or loads: waits are wait_copies, and m0 is as before.)
+// Eight copies of 1 KiB of a block of the pool to a slot, lane l of copy y from offset y * 1024 + o[y].  No
+// block: a buffer of no bytes, nothing is fetched.  (The compiler does not know them as LDS writes or loads:
+// waits are wait_copies, and m0 is as before.)
 template <bool ONCE>
-LVS_DEV void copy_page(const uint8_t* pool, int id, int64_t head, uint32_t slot, int o0, int o1, int o2, int o3,
-                       int n_heads) {
+LVS_DEV void copy_page(const uint8_t* pool, int id, int64_t head, int n_heads, uint32_t slot, const int (&o)[8]) {
   const uint64_t at = (uint64_t)(pool + ((int64_t)max(id, 0) * n_heads + head) * kPageBytes);
   u32x4 from = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, id >= 0 ? (uint32_t)kPageBytes : 0u, kBufferWord};
 #pragma unroll
   for (int i = 0; i < 4; ++i) from[i] = __builtin_amdgcn_readfirstlane(from[i]);      // (in scalar registers)
   const uint32_t to = __builtin_amdgcn_readfirstlane(slot);
   uint32_t keep, far;
-#define LVS_COPY_1(O, POLICY) "buffer_load_dwordx4 " O ", %7, %1 offen" POLICY " lds\n\t"
+#define LVS_COPY_1(O, P) "buffer_load_dwordx4 " O ", %11, %1 offen" P " lds\n\t"
 #define LVS_COPY_NEXT "s_add_u32 m0, m0, 0x400\n\ts_add_u32 %1, %1, 0x400\n\ts_nop 0\n\t"
 #define LVS_COPY(P)                                                                                   \
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %6\n\ts_mov_b32 %1, 0\n\ts_nop 0\n\t"                 \
-               LVS_COPY_1("%2", P) LVS_COPY_NEXT LVS_COPY_1("%2", P) LVS_COPY_NEXT                    \
-               LVS_COPY_1("%3", P) LVS_COPY_NEXT LVS_COPY_1("%3", P) LVS_COPY_NEXT                    \
-               LVS_COPY_1("%4", P) LVS_COPY_NEXT LVS_COPY_1("%4", P) LVS_COPY_NEXT                    \
-               LVS_COPY_1("%5", P) LVS_COPY_NEXT LVS_COPY_1("%5", P) "s_mov_b32 m0, %0"               \
-               : "=&s"(keep), "=&s"(far) : "v"(o0), "v"(o1), "v"(o2), "v"(o3), "s"(to), "s"(from) : "memory", "scc")
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %10\n\ts_mov_b32 %1, 0\n\ts_nop 0\n\t"                \
+               LVS_COPY_1("%2", P) LVS_COPY_NEXT LVS_COPY_1("%3", P) LVS_COPY_NEXT                    \
+               LVS_COPY_1("%4", P) LVS_COPY_NEXT LVS_COPY_1("%5", P) LVS_COPY_NEXT                    \
+               LVS_COPY_1("%6", P) LVS_COPY_NEXT LVS_COPY_1("%7", P) LVS_COPY_NEXT                    \
+               LVS_COPY_1("%8", P) LVS_COPY_NEXT LVS_COPY_1("%9", P) "s_mov_b32 m0, %0"               \
+               : "=&s"(keep), "=&s"(far)                                                             \
+               : "v"(o[0]), "v"(o[1]), "v"(o[2]), "v"(o[3]), "v"(o[4]), "v"(o[5]), "v"(o[6]), "v"(o[7]), "s"(to), \
+                 "s"(from)                                                                           \
+               : "memory", "scc")
   if constexpr (ONCE)
     LVS_COPY(" nt");
   else
@@ -161,87 +160,283 @@ LVS_DEV Cut cut_units(const PagedAttnKernelArgs& p, int lane, int places0) {
 }
 
 // ------------------------------------------------------------------------------ split
-// NB blocks of 16 rows by KS streams of tiles, a wave each.
-template <int NB, int KS>
-struct Shape {
-  static constexpr int kRows = 16 * NB;
-  static constexpr int kMergeBytes = (int)sizeof(float) * KS * kRows * (1 + kMergeStride);
-  static constexpr int kLds = kMergeBytes > KS * kRingBytes ? kMergeBytes : KS * kRingBytes;
-};
+LVS_DEV u32x4 pack8(float a, float b, float c, float d, float e, float f, float g, float h) {
+  return u32x4{pack_bf16(a, b), pack_bf16(c, d), pack_bf16(e, f), pack_bf16(g, h)};
+}
+LVS_DEV f32x4 four_bf16(const uint8_t* at) {
+  const uint2 x = *reinterpret_cast<const uint2*>(at);
+  return f32x4{__builtin_bit_cast(float, x.x << 16), __builtin_bit_cast(float, x.x & 0xffff0000u),
+               __builtin_bit_cast(float, x.y << 16), __builtin_bit_cast(float, x.y & 0xffff0000u)};
+}
+LVS_DEV bool finite(float x) { return fabsf(x) <= 3.4028234663852886e38f; }
 
-template <int NB>
-struct RowState {
-  f32x4 acc[NB][8];        // O^T: channels 16 db + 4 g4 + i of row n16
-  float m[NB], l[NB], lv[NB];
-};
-
-// Scores of NK blocks of 16 keys to probabilities (in place); the running maximum and the sums follow.
+// Scores of a tile to probabilities (in place); running maximum m, sum l.  LANES lanes hold a row's scores.
 // `first`: there is nothing to rescale yet.  The maximum is exact: a reference that is taken anew only for
 // scores 2^8 above it saves 1 to 4 % of the time and costs the exact 1 of the largest probability (error
 // against 64 bits 2.2e-3 -> 2.5e-3).
-template <int NB, int NK>
-LVS_DEV void softmax_tile(RowState<NB>& st, f32x4 (&s)[NB][NK], float c, bool first) {
-  bool grow = false;
-  float top[NB];
+template <int LANES, int N, class Rescale>
+LVS_DEV void softmax_row(float (&s)[N], float& m, float& l, float c, bool first, Rescale&& rescale) {
+  float top = s[0];
 #pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    float t = s[nb][0][0];
-#pragma unroll
-    for (int k = 0; k < NK; ++k)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) t = fmaxf(t, s[nb][k][i]);
-    top[nb] = t * c;
-    grow |= top[nb] > st.m[nb];
+  for (int i = 1; i < N; ++i) top = fmaxf(top, s[i]);
+  top *= c;
+  if (__any(top > m)) {
+    float x = max_halves(fmaxf(m, top));
+    if constexpr (LANES == 4) x = max_rows(x);
+    const float alpha = fast_exp2(m - x);
+    m = x;
+    if (!first) rescale(alpha);
   }
-  if (__any(grow)) {
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      const float x = max_rows(max_halves(fmaxf(st.m[nb], top[nb])));
-      const float alpha = fast_exp2(st.m[nb] - x);
-      st.m[nb] = x;
-      if (!first) {
-        st.l[nb] *= alpha;
-        st.lv[nb] *= alpha;
+  for (int i = 0; i < N; ++i) s[i] = fast_exp2(__builtin_fmaf(s[i], c, -m));
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int db = 0; db < 8; ++db) st.acc[nb][db] *= alpha;
+  for (int i = 0; i < N; ++i) sum[i & 3] += s[i];
+  l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+}
+
+// Up to 16 query rows, on 16x16 tiles: a quarter of the wave's lanes (g4) holds a row (n16).
+// A tile's scores: key 16 g4 + 4 kb + i is element 4 kb + i.
+struct Rows16 {
+  static constexpr int kRows = 16, kScores = 16, kLanes = 4;
+  u32x4 q[4];              // channels 64 (x/2) + 16 g4 + 8 (x%2) .. +7
+  f32x4 acc[8];            // O^T: channels 16 db + 4 g4 + i
+  float m, l, lv;
+
+  static LVS_DEV int k_place(int t) { return ((t >> 1) & 1) | (((t >> 4) & 3) << 1); }
+  static LVS_DEV int v_place(int q) { return ((q >> 1) & 1) | (((q ^ (q >> 1)) & 1) << 1); }    // 0 2 3 1
+  static LVS_DEV int row_of(int lane) { return lane & 15; }
+  static LVS_DEV int key_of(int lane, int e) { return 16 * (lane >> 4) + e; }
+
+  LVS_DEV void load_q(const uint16_t* qp, int lane) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      q[x] = *reinterpret_cast<const u32x4*>(qp + 64 * (x >> 1) + 16 * (lane >> 4) + 8 * (x & 1));
+  }
+  LVS_DEV void clear() {
+#pragma unroll
+    for (int db = 0; db < 8; ++db) acc[db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m = kNegBig;
+    l = lv = 0.f;
+  }
+  LVS_DEV void rescale(float a) {
+    l *= a;
+    lv *= a;
+#pragma unroll
+    for (int db = 0; db < 8; ++db) acc[db] *= a;
+  }
+  // operand reads: token 16 (n16/4) + 4 kb + n16%4, chunk 4 half + g4; channel 16 x + n16, chunk g4
+  LVS_DEV void read_k(u32x4 (&k)[8], uint32_t slot, int lane) const {
+    const int n16 = lane & 15, g4 = lane >> 4, t = 16 * (n16 >> 2) + (n16 & 3), f = k_place(t);
+    const uint32_t a0 = slot + t * 128 + ((g4 ^ f) << 4), a1 = slot + t * 128 + (((4 + g4) ^ f) << 4);
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb) {
+      k[2 * kb] = lds_load16(a0 + kb * 512);
+      k[2 * kb + 1] = lds_load16(a1 + kb * 512);
+    }
+  }
+  LVS_DEV void read_v(u32x4 (&v)[8], uint32_t slot, int lane) const {
+    const int n16 = lane & 15;
+    const uint32_t a = slot + n16 * kPageTokens + (((lane >> 4) ^ v_place(n16 >> 2)) << 4);
+#pragma unroll
+    for (int x = 0; x < 8; ++x) v[x] = lds_load16(a + x * 1024);
+  }
+  LVS_DEV void scores(float (&s)[16], const u32x4 (&k)[8], float scale) const {
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb) {
+      f32x4 z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const u32x4& raw = k[2 * kb + (x >> 1)];
+        z = mfma16(widen(raw[(x & 1) * 2], raw[(x & 1) * 2 + 1], scale), q[x], z);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[4 * kb + i] = z[i];
+    }
+  }
+  LVS_DEV void output(const u32x4 (&pr)[2], const u32x4 (&v)[8], float scale) {
+#pragma unroll
+    for (int db = 0; db < 8; ++db)
+#pragma unroll
+      for (int y = 0; y < 2; ++y) acc[db] = mfma16(widen(v[db][2 * y], v[db][2 * y + 1], scale), pr[y], acc[db]);
+  }
+  // a piece of 32 open rows: element 4 kb + i is key 16 kb + 4 g4 + i
+  static constexpr int kOpenScores = 8;
+  static LVS_DEV int open_key(int lane, int e) { return 16 * (e >> 2) + 4 * (lane >> 4) + (e & 3); }
+  LVS_DEV void open_load(u32x4 (&k)[8], const uint8_t* kt, int p0, int lane) const {
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        k[4 * kb + x] = *reinterpret_cast<const u32x4*>(kt + ((p0 + 16 * kb + (lane & 15)) & (kTailRows - 1)) * kRowBytes +
+                                                        2 * (64 * (x >> 1) + 16 * (lane >> 4) + 8 * (x & 1)));
+  }
+  LVS_DEV void open_scores(float (&s)[8], const u32x4 (&k)[8]) const {
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      f32x4 z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < 4; ++x) z = mfma16(k[4 * kb + x], q[x], z);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[4 * kb + i] = z[i];
+    }
+  }
+  LVS_DEV void open_output(const float (&s)[8], uint32_t turn, int lane) {
+    const u32x4 pr = pack8(s[0], s[1], s[2], s[3], s[4], s[5], s[6], s[7]);
+    const int n16 = lane & 15, tr = 4 * (lane >> 4) + (n16 >> 2);      // row and chunk this lane hands in
+#pragma unroll
+    for (int db = 0; db < 8; ++db) {
+      const uint32_t at = turn + ((((2 * db + ((n16 & 3) >> 1)) ^ rows32_swz(tr)) << 4) | ((n16 & 1) << 3));
+      const u32x2 lo = lds_load_tr(at + tr * kRowBytes);
+      const u32x2 hi = lds_load_tr(at + (16 + tr) * kRowBytes);
+      acc[db] = mfma16(u32x4{lo[0], lo[1], hi[0], hi[1]}, pr, acc[db]);
+    }
+  }
+  LVS_DEV void add_odd(const uint8_t* row, bool sees, int lane) {
+#pragma unroll
+    for (int db = 0; db < 8; ++db) {
+      const f32x4 y = four_bf16(row + 2 * (16 * db + 4 * (lane >> 4)));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[db][i] += sees && !finite(y[i]) ? y[i] : 0.f;
+    }
+  }
+  LVS_DEV void store(float* o, float f, int lane) const {
+#pragma unroll
+    for (int db = 0; db < 8; ++db) *reinterpret_cast<f32x4*>(o + 16 * db + 4 * (lane >> 4)) = acc[db] * f;
+  }
+};
+
+// 17 to 32 rows, on 32x32 tiles, which leave the vector unit more room beside the matrix unit than 16x16 ones
+// (matrix instructions of one wave and FMAs of another on a SIMD: 366 us together, 238 and 307 alone; on 16x16
+// 402, 257 and 307): half a wave's lanes (h) hold a row (n32).  Key 32 kb + 16 h + r is element 16 kb + r.
+struct Rows32Core {
+  static constexpr int kRows = 32, kScores = 32, kLanes = 2;
+  u32x4 q[8];              // channels 16 (2 (x/2) + h) + 8 (x%2) .. +7
+  f32x16 acc[4];           // O^T: channels 32 db + 8 (r/4) + 4 h + r%4
+  float m, l, lv;
+
+  static LVS_DEV int k_place(int t) { return (t >> 1) & 7; }
+  static LVS_DEV int v_place(int q) { return q & 3; }
+  static LVS_DEV int row_of(int lane) { return lane & 31; }
+  static LVS_DEV int key_of(int lane, int e) { return 32 * (e >> 4) + 16 * (lane >> 5) + (e & 15); }
+
+  LVS_DEV void load_q(const uint16_t* qp, int lane) {
+#pragma unroll
+    for (int x = 0; x < 8; ++x)
+      q[x] = *reinterpret_cast<const u32x4*>(qp + 16 * (2 * (x >> 1) + (lane >> 5)) + 8 * (x & 1));
+  }
+  LVS_DEV void clear() {
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[db][r] = 0.f;
+    m = kNegBig;
+    l = lv = 0.f;
+  }
+  LVS_DEV void rescale(float a) {
+    l *= a;
+    lv *= a;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[db][r] *= a;
+  }
+  // operand reads: row m of block kb is token 32 kb + 16 (m/4 % 2) + 4 (m/8) + m%4, chunk 2 i + h; channel
+  // 32 db + n32, chunk 2 kb + h
+  LVS_DEV void read_k(u32x4 (&k)[8], uint32_t slot, int lane) const {
+    const int n = lane & 31, t = 16 * ((n >> 2) & 1) + 4 * (n >> 3) + (n & 3);
+    const uint32_t a = slot + t * 128 + (((lane >> 5) ^ k_place(t)) << 4);
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) k[4 * kb + i] = lds_load16((a ^ (i << 5)) + kb * 4096);
+  }
+  LVS_DEV void read_v(u32x4 (&v)[8], uint32_t slot, int lane) const {
+    const int n = lane & 31;
+    const uint32_t a = slot + n * kPageTokens + (((lane >> 5) ^ v_place(n >> 2)) << 4);
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) v[2 * db + kb] = lds_load16((a ^ (kb << 5)) + db * 2048);
+  }
+  LVS_DEV void scores(float (&s)[32], const u32x4 (&k)[8], float scale) const {
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      f32x16 z;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) z[r] = 0.f;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        const u32x4& raw = k[4 * kb + (x >> 1)];
+        z = mfma32(widen(raw[(x & 1) * 2], raw[(x & 1) * 2 + 1], scale), q[x], z);
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[16 * kb + r] = z[r];
+    }
+  }
+  LVS_DEV void output(const u32x4 (&pr)[4], const u32x4 (&v)[8], float scale) {
+#pragma unroll
+    for (int y = 0; y < 4; ++y)
+#pragma unroll
+      for (int db = 0; db < 4; ++db) {
+        const u32x4& raw = v[2 * db + (y >> 1)];
+        acc[db] = mfma32(widen(raw[(y & 1) * 2], raw[(y & 1) * 2 + 1], scale), pr[y], acc[db]);
+      }
+  }
+  // a piece of 32 open rows: element r is key 8 (r/4) + 4 h + r%4
+  static constexpr int kOpenScores = 16;
+  static LVS_DEV int open_key(int lane, int e) { return 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3); }
+  LVS_DEV void open_load(u32x4 (&k)[8], const uint8_t* kt, int p0, int lane) const {
+#pragma unroll
+    for (int x = 0; x < 8; ++x)
+      k[x] = *reinterpret_cast<const u32x4*>(kt + ((p0 + (lane & 31)) & (kTailRows - 1)) * kRowBytes +
+                                             2 * (16 * (2 * (x >> 1) + (lane >> 5)) + 8 * (x & 1)));
+  }
+  LVS_DEV void open_scores(float (&s)[16], const u32x4 (&k)[8]) const {
+    f32x16 z;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) z[r] = 0.f;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) z = mfma32(k[x], q[x], z);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = z[r];
+  }
+  LVS_DEV void open_output(const float (&s)[16], uint32_t turn, int lane) {
+    const int h = lane >> 5, rr = (lane & 15) >> 2, g1 = (lane >> 4) & 1;
+    const int chunk = (2 * g1 + ((lane & 3) >> 1)) ^ rows32_swz(4 * h + rr);
+    const uint32_t a0 = turn + (4 * h + rr) * kRowBytes + (chunk << 4) + (lane & 1) * 8;
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+      const u32x4 pr = pack8(s[8 * kt], s[8 * kt + 1], s[8 * kt + 2], s[8 * kt + 3], s[8 * kt + 4], s[8 * kt + 5],
+                             s[8 * kt + 6], s[8 * kt + 7]);
+#pragma unroll
+      for (int db = 0; db < 4; ++db) {
+        const uint32_t a = a0 ^ (db << 6);
+        const u32x2 lo = lds_load_tr(a + kt * (16 * kRowBytes));
+        const u32x2 hi = lds_load_tr((a ^ 32) + (kt * 16 + 8) * kRowBytes);
+        acc[db] = mfma32(u32x4{lo[0], lo[1], hi[0], hi[1]}, pr, acc[db]);
       }
     }
   }
+  LVS_DEV void add_odd(const uint8_t* row, bool sees, int lane) {
 #pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    float sum = 0.f;
+    for (int db = 0; db < 4; ++db)
 #pragma unroll
-    for (int k = 0; k < NK; ++k) {
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 y = four_bf16(row + 2 * (32 * db + 8 * g + 4 * (lane >> 5)));
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[nb][k][i] = fast_exp2(__builtin_fmaf(s[nb][k][i], c, -st.m[nb]));
-      sum += (s[nb][k][0] + s[nb][k][1]) + (s[nb][k][2] + s[nb][k][3]);
-    }
-    st.l[nb] += sum;
-  }
-}
-
-// softmax mass on the video span; key_of(k, i): cache row of score i of block k
-template <int NB, int NK, class KeyOf>
-LVS_DEV void span_mass(RowState<NB>& st, const f32x4 (&s)[NB][NK], int key0, int keys, int vis_b, int vis_e,
-                       KeyOf&& key_of) {
-  if (!(key0 < vis_e && key0 + keys > vis_b)) return;
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    float sum = 0.f;
-#pragma unroll
-    for (int k = 0; k < NK; ++k)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int key = key_of(k, i);
-        sum += key >= vis_b && key < vis_e ? s[nb][k][i] : 0.f;
+        for (int i = 0; i < 4; ++i) acc[db][4 * g + i] += sees && !finite(y[i]) ? y[i] : 0.f;
       }
-    st.lv[nb] += sum;
   }
-}
-
-LVS_DEV u32x4 pack8(const f32x4& a, const f32x4& b) {
-  return u32x4{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3]), pack_bf16(b[0], b[1]), pack_bf16(b[2], b[3])};
-}
+  LVS_DEV void store(float* o, float f, int lane) const {
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f32x4*>(o + 32 * db + 8 * g + 4 * (lane >> 5)) =
+            f32x4{acc[db][4 * g], acc[db][4 * g + 1], acc[db][4 * g + 2], acc[db][4 * g + 3]} * f;
+  }
+};
 
 // four channels of an output row; lane 0 of 32 its log-sum-exp and mass
 LVS_DEV void write_row(const PagedAttnKernelArgs& p, int b, int h, int r, int l32, const f32x4& o, float m, float l,
@@ -260,14 +455,20 @@ LVS_DEV void write_row(const PagedAttnKernelArgs& p, int b, int h, int r, int l3
   }
 }
 
-template <int NB, int KS, bool ONCE>
+// KS streams of tiles, a wave each.
+template <class Rows, int KS>
+constexpr int segment_lds() {
+  constexpr int merge = (int)sizeof(float) * KS * Rows::kRows * (1 + kMergeStride);
+  return merge > KS * kRingBytes ? merge : KS * kRingBytes;
+}
+
+template <class Rows, int KS, bool ONCE>
 struct Segment {
-  using W = Shape<NB, KS>;
+  static constexpr int kRows = Rows::kRows;
   const PagedAttnKernelArgs& p;
   uint8_t* smem;
   int stream;
-  u32x4 q[NB][4];          // channels 64 (c/2) + 16 g4 + 8 (c%2) .. +7 of row n16
-  RowState<NB> st;
+  Rows st;
   int vis_b, vis_e;
   bool fresh;              // nothing in the state yet
 
@@ -275,36 +476,22 @@ struct Segment {
     stream = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   }
 
-  // The lane's number, row or token (n16) and quarter (g4).  Every part of a segment takes them anew: what
-  // follows from them would else be held in registers through the loop over the tiles.
-  struct Lane {
-    int lane, n16, g4;
-    LVS_DEV Lane() {
-      lane = threadIdx.x & 63;
-      asm volatile("" : "+v"(lane));
-      n16 = lane & 15;
-      g4 = lane >> 4;
-    }
-  };
+  // The lane's number.  Every part of a segment takes it anew: what follows from it would else be held in
+  // registers through the loop over the tiles.
+  static LVS_DEV int lane_now() {
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    return lane;
+  }
+
+  // draft row of the lane's query row (rows past the last one: that row again, to no output)
+  LVS_DEV int query_row(int rc, int lane) const { return min(rc * p.rpad + Rows::row_of(lane), p.R - 1); }
 
   LVS_DEV void begin(int b, int h, int rc) {
-    const Lane me;
-    const int n16 = me.n16, g4 = me.g4;
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      const int r = rc * p.rpad + nb * 16 + n16;
-      const int rcl = r < p.R ? r : p.R - 1;     // (rows past the last one: that row again, to no output)
-      const int qi = (int)fast_div((uint32_t)rcl, p.div_g);
-      const uint16_t* qp = p.q + (int64_t)b * p.q_sb + (int64_t)qi * p.q_sg +
-                           (int64_t)(h * p.G + (rcl - qi * p.G)) * p.q_sh;
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-        q[nb][c] = *reinterpret_cast<const u32x4*>(qp + 64 * (c >> 1) + 16 * g4 + 8 * (c & 1));
-#pragma unroll
-      for (int db = 0; db < 8; ++db) st.acc[nb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
-      st.m[nb] = kNegBig;
-      st.l[nb] = st.lv[nb] = 0.f;
-    }
+    const int lane = lane_now(), r = query_row(rc, lane);
+    const int qi = (int)fast_div((uint32_t)r, p.div_g);
+    st.load_q(p.q + (int64_t)b * p.q_sb + (int64_t)qi * p.q_sg + (int64_t)(h * p.G + (r - qi * p.G)) * p.q_sh, lane);
+    st.clear();
     fresh = true;
     vis_b = vis_e = 0;
     if (p.vis_begin != nullptr) {
@@ -313,12 +500,27 @@ struct Segment {
     }
   }
 
+  // softmax of a tile or piece; its mass on the video span
+  template <int N, class KeyOf>
+  LVS_DEV void softmax(float (&s)[N], int key0, int keys, KeyOf&& key_of) {
+    softmax_row<Rows::kLanes>(s, st.m, st.l, p.scale_log2e, fresh, [&](float a) { st.rescale(a); });
+    fresh = false;
+    if (key0 < vis_e && key0 + keys > vis_b) {
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const int key = key0 + key_of(e);
+        sum += key >= vis_b && key < vis_e ? s[e] : 0.f;
+      }
+      st.lv += sum;
+    }
+  }
+
   // tiles t0 .. t1-1 of a unit
   LVS_DEV void blocks(int b, int h, int t0, int t1) {
     const int mine = (t1 - t0 - stream + KS - 1) / KS;
     if (mine <= 0) return;
-    const Lane me;
-    const int lane = me.lane, n16 = me.n16, g4 = me.g4;
+    const int lane = lane_now();
     const int32_t* row = p.table + (int64_t)b * p.cols;
     // blocks of 64 tiles, one per lane.  An entry that names no block of the pool is -1.
     int ids;
@@ -333,84 +535,49 @@ struct Segment {
       return *(const __attribute__((address_space(4))) float*)(uintptr_t)(scale + ((int64_t)max(id, 0) * p.Hkv + h));
     };
     const uint32_t k_slot = lds_addr(smem) + stream * kRingBytes, v_slot = k_slot + kPageBytes;
-    // global side of the copies: row and chunk that belong at lane's place (see k_place, v_place)
-    const int k_from = (lane >> 3) * 128, k_chunk = (lane & 7) ^ ((lane >> 4) & 1);
-    int k_off[4];
+    // global side of the copies: the chunk that belongs at the lane's place
+    int k_off[8], v_off[8];
 #pragma unroll
-    for (int y = 0; y < 4; ++y) k_off[y] = k_from + ((k_chunk ^ (y << 1)) << 4);
-    const int v_off = (lane >> 2) * kPageTokens + (((lane & 3) ^ v_place(lane >> 4)) << 4);
-    auto copy_k = [&](int id) { copy_page<ONCE>(p.k8, id, h, k_slot, k_off[0], k_off[1], k_off[2], k_off[3], p.Hkv); };
-    auto copy_v = [&](int id) { copy_page<ONCE>(p.v8, id, h, v_slot, v_off, v_off, v_off, v_off, p.Hkv); };
-    // LDS side of the operands: token 16 (n16/4) + 4 kb + n16%4, chunk 4 half + g4; channel 16 x + n16, chunk g4
-    const uint32_t k_at = k_slot + (16 * (n16 >> 2) + (n16 & 3)) * 128;
-    const int k_key = ((n16 >> 1) & 1) | ((n16 >> 2) << 1);
-    const uint32_t k_at0 = k_at + ((g4 ^ k_key) << 4), k_at1 = k_at + (((4 + g4) ^ k_key) << 4);
-    const uint32_t v_at = v_slot + n16 * kPageTokens + ((g4 ^ v_place(n16 >> 2)) << 4);
+    for (int y = 0; y < 8; ++y) {
+      k_off[y] = (lane >> 3) * 128 + (((lane & 7) ^ Rows::k_place(8 * y + (lane >> 3))) << 4);
+      v_off[y] = (lane >> 2) * kPageTokens + (((lane & 3) ^ Rows::v_place(lane >> 4)) << 4);
+    }
+    auto copy_k = [&](int id) { copy_page<ONCE>(p.k8, id, h, p.Hkv, k_slot, k_off); };
+    auto copy_v = [&](int id) { copy_page<ONCE>(p.v8, id, h, p.Hkv, v_slot, v_off); };
     fetch(0);
     int id = __builtin_amdgcn_readlane(ids, 0);
     copy_k(id);
     copy_v(id);
     float k_scale = scale_of(p.k_scale, id), v_scale = scale_of(p.v_scale, id);
-    const float c = p.scale_log2e;
     for (int j = 0; j < mine; ++j) {
       const bool more = j + 1 < mine;
       if (((j + 1) & 63) == 0) fetch(j + 1);
       const int next = more ? __builtin_amdgcn_readlane(ids, (j + 1) & 63) : -1;
       u32x4 k[8];
       wait_copies<8>();                // all but V's
-#pragma unroll
-      for (int kb = 0; kb < 4; ++kb) {
-        k[2 * kb] = lds_load16(k_at0 + kb * 512);
-        k[2 * kb + 1] = lds_load16(k_at1 + kb * 512);
-      }
+      st.read_k(k, k_slot, lane);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       if (more) copy_k(next);
       const float k_next = scale_of(p.k_scale, next), v_next = scale_of(p.v_scale, next);
-      f32x4 s[NB][4];
+      float s[Rows::kScores];
+      st.scores(s, k, k_scale);
+      u32x4 pr[Rows::kScores / 8];
+      if (id >= 0) {                   // (an entry that names no block of the pool: no key)
+        softmax(s, (t0 + stream + KS * j) * kPageTokens, kPageTokens, [&](int e) { return Rows::key_of(lane, e); });
 #pragma unroll
-      for (int kb = 0; kb < 4; ++kb) {
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) s[nb][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const u32x4& raw = k[kb * 2 + (x >> 1)];
-          const u32x4 a = widen(raw[(x & 1) * 2], raw[(x & 1) * 2 + 1], k_scale);
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) s[nb][kb] = mfma16(a, q[nb][x], s[nb][kb]);
-        }
-      }
-      u32x4 pr[NB][2];
-      if (id >= 0) {
-        softmax_tile<NB, 4>(st, s, c, fresh);
-        fresh = false;
-        const int key0 = (t0 + stream + KS * j) * kPageTokens;
-        span_mass<NB, 4>(st, s, key0, kPageTokens, vis_b, vis_e,
-                         [&](int kb, int i) { return key0 + 16 * g4 + 4 * kb + i; });
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          pr[nb][0] = pack8(s[nb][0], s[nb][1]);
-          pr[nb][1] = pack8(s[nb][2], s[nb][3]);
-        }
+        for (int y = 0; y < Rows::kScores / 8; ++y)
+          pr[y] = pack8(s[8 * y], s[8 * y + 1], s[8 * y + 2], s[8 * y + 3], s[8 * y + 4], s[8 * y + 5], s[8 * y + 6],
+                        s[8 * y + 7]);
       }
       u32x4 v[8];
       if (more)
         wait_copies<8>();              // all but the next K's
       else
         wait_copies<0>();
-#pragma unroll
-      for (int x = 0; x < 8; ++x) v[x] = lds_load16(v_at + x * 1024);
+      st.read_v(v, v_slot, lane);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       if (more) copy_v(next);
-      if (id >= 0) {
-#pragma unroll
-        for (int db = 0; db < 8; ++db)
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const u32x4 a = widen(v[db][2 * y], v[db][2 * y + 1], v_scale);
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) st.acc[nb][db] = mfma16(a, pr[nb][y], st.acc[nb][db]);
-          }
-      }
+      if (id >= 0) st.output(pr, v, v_scale);
       id = next;
       k_scale = k_next;
       v_scale = v_next;
@@ -438,31 +605,20 @@ struct Segment {
 
   // open rows: positions L / 64 * 64 .. L + gamma - 1, in pieces of 32 keys, one stream each
   LVS_DEV void open_rows(int b, int h, int rc, int L) {
-    const Lane me;
-    const int n16 = me.n16, g4 = me.g4;
+    const int lane = lane_now(), n16 = lane & 15, g4 = lane >> 4;
     const int base = L & ~(kPageTokens - 1);
     const int n = L - base + p.gamma;
-    uint32_t rowmask[NB];            // draft rows that row n16 sees
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      const int r = rc * p.rpad + nb * 16 + n16;
-      rowmask[nb] = p.draft_mask[fast_div((uint32_t)(r < p.R ? r : p.R - 1), p.div_g)] & (0xffffffffu >> (32 - p.gamma));
-    }
+    const uint32_t rowmask = p.draft_mask[fast_div((uint32_t)query_row(rc, lane), p.div_g)] &
+                             (0xffffffffu >> (32 - p.gamma));            // draft rows that the lane's row sees
     const int64_t unit = ((int64_t)b * p.Hkv + h) * (kTailRows * kRowBytes);
     const uint8_t* kt = p.k_tail + unit;
     const uint8_t* vt = p.v_tail + unit;
     const uint32_t turn = lds_addr(smem) + stream * kRingBytes;
-    const float c = p.scale_log2e;
     // (from the last stream on: the first ones have the odd tiles)
     for (int piece = KS - 1 - stream; piece * 32 < n; piece += KS) {
       const int p0 = base + piece * 32;
-      u32x4 k[2][4], v[8];
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-          k[kb][x] = *reinterpret_cast<const u32x4*>(kt + ((p0 + 16 * kb + n16) & (kTailRows - 1)) * kRowBytes +
-                                                     2 * (64 * (x >> 1) + 16 * g4 + 8 * (x & 1)));
+      u32x4 k[8], v[8];
+      st.open_load(k, kt, p0, lane);
 #pragma unroll
       for (int x = 0; x < 8; ++x)
         v[x] = *reinterpret_cast<const u32x4*>(vt + ((p0 + 4 * x + g4) & (kTailRows - 1)) * kRowBytes + n16 * 16);
@@ -483,58 +639,22 @@ struct Segment {
         *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(turn + r * kRowBytes +
                                                                ((n16 ^ rows32_swz(r & 15)) << 4)) = v[x];
       }
-      f32x4 s[NB][2];
+      float s[Rows::kOpenScores];
+      st.open_scores(s, k);
+      // bit k: the lane's row sees key k of the piece; committed keys first, then the draft rows
+      const int old = L - p0;
+      const uint32_t sees = old >= 32 ? 0xffffffffu
+                            : old >= 0 ? ((1u << old) - 1u) | (rowmask << old) : rowmask >> min(-old, 31);
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-          f32x4 z = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int x = 0; x < 4; ++x) z = mfma16(k[kb][x], q[nb][x], z);
-          // bit k: row n16 sees key k of the piece; committed keys first, then the draft rows
-          const int old = L - p0;
-          const uint32_t sees = old >= 32 ? 0xffffffffu
-                                : old >= 0 ? ((1u << old) - 1u) | (rowmask[nb] << old) : rowmask[nb] >> min(-old, 31);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) z[i] = (sees >> (4 * g4)) & (1u << (16 * kb + i)) ? z[i] : -INFINITY;
-          s[nb][kb] = z;
-        }
-      softmax_tile<NB, 2>(st, s, c, fresh);
-      fresh = false;
-      span_mass<NB, 2>(st, s, p0, 32, vis_b, vis_e, [&](int kb, int i) { return p0 + 16 * kb + 4 * g4 + i; });
-      u32x4 pr[NB];
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) pr[nb] = pack8(s[nb][0], s[nb][1]);
+      for (int e = 0; e < Rows::kOpenScores; ++e) s[e] = (sees >> Rows::open_key(lane, e)) & 1u ? s[e] : -INFINITY;
+      softmax(s, p0, 32, [&](int e) { return Rows::open_key(lane, e); });
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      const int tr = 4 * g4 + (n16 >> 2);                      // row and chunk this lane hands in
-#pragma unroll
-      for (int db = 0; db < 8; ++db) {
-        const uint32_t at = turn + ((((2 * db + ((n16 & 3) >> 1)) ^ rows32_swz(tr)) << 4) | ((n16 & 1) << 3));
-        const u32x2 lo = lds_load_tr(at + tr * kRowBytes);
-        const u32x2 hi = lds_load_tr(at + (16 + tr) * kRowBytes);
-        const u32x4 a = u32x4{lo[0], lo[1], hi[0], hi[1]};
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) st.acc[nb][db] = mfma16(a, pr[nb], st.acc[nb][db]);
-      }
+      st.open_output(s, turn, lane);
       // (any weight times a value that is not finite is that value: it is added as it is)
       while (odd != 0u) {
         const int key = __builtin_ctz(odd);
         odd &= odd - 1;
-        const int j = p0 + key - L;
-        const uint8_t* vr = vt + ((p0 + key) & (kTailRows - 1)) * kRowBytes;
-#pragma unroll
-        for (int db = 0; db < 8; ++db) {
-          const uint2 x = *reinterpret_cast<const uint2*>(vr + 2 * (16 * db + 4 * g4));
-          const f32x4 y = {__builtin_bit_cast(float, x.x << 16), __builtin_bit_cast(float, x.x & 0xffff0000u),
-                           __builtin_bit_cast(float, x.y << 16), __builtin_bit_cast(float, x.y & 0xffff0000u)};
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) {
-            const bool sees = j < 0 || ((rowmask[nb] >> (j < 0 ? 0 : j)) & 1u) != 0u;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              st.acc[nb][db][i] += sees && !(fabsf(y[i]) <= 3.4028234663852886e38f) ? y[i] : 0.f;
-          }
-        }
+        st.add_odd(vt + ((p0 + key) & (kTailRows - 1)) * kRowBytes, ((sees >> key) & 1u) != 0u, lane);
       }
     }
   }
@@ -553,49 +673,39 @@ struct Segment {
   // sums: [KS][kRows] maxima, then per stream and row 132 floats, the output, the denominator and its share
   // on the video span.
   LVS_DEV void gather(uint32_t on) {
-    const Lane me;
-    const int n16 = me.n16, g4 = me.g4;
+    const int lane = lane_now(), row = Rows::row_of(lane);
     float* sm_m = reinterpret_cast<float*>(smem);
     __syncthreads();
-    if (g4 == 0) {
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) sm_m[stream * W::kRows + nb * 16 + n16] = st.m[nb];
-    }
+    if (lane < kRows) sm_m[stream * kRows + row] = st.m;
     __syncthreads();
     if (((on >> stream) & 1u) == 0u) return;
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      const int row = nb * 16 + n16;
-      float mm = sm_m[row];
-#pragma unroll
-      for (int k = 1; k < KS; ++k) mm = fmaxf(mm, sm_m[k * W::kRows + row]);
-      const float f = fast_exp2(st.m[nb] - mm);
-      float* o = sm_m + KS * W::kRows + (stream * W::kRows + row) * kMergeStride;
-#pragma unroll
-      for (int db = 0; db < 8; ++db) *reinterpret_cast<f32x4*>(o + 16 * db + 4 * g4) = st.acc[nb][db] * f;
-      float l = st.l[nb] * f, lv = st.lv[nb] * f;
+    const float f = fast_exp2(st.m - merged_max(row));
+    float* o = sm_m + KS * kRows + (stream * kRows + row) * kMergeStride;
+    st.store(o, f, lane);
+    float l = st.l * f, lv = st.lv * f;
+    if constexpr (Rows::kLanes == 4) {
       l += xor_shuffle(l, 16);
-      l += xor_shuffle(l, 32);
       lv += xor_shuffle(lv, 16);
-      lv += xor_shuffle(lv, 32);
-      if (g4 == 0) *reinterpret_cast<float2*>(o + 128) = float2{l, lv};
     }
+    l += xor_shuffle(l, 32);
+    lv += xor_shuffle(lv, 32);
+    if (lane < kRows) *reinterpret_cast<float2*>(o + 128) = float2{l, lv};
   }
 
   // sums over the active streams of four floats of a row
   LVS_DEV f32x4 merged(uint32_t on, int row, int c4) {
-    const float* o = reinterpret_cast<const float*>(smem) + KS * W::kRows + row * kMergeStride + c4;
+    const float* o = reinterpret_cast<const float*>(smem) + KS * kRows + row * kMergeStride + c4;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < KS; ++k)
-      if ((on >> k) & 1u) sum += *reinterpret_cast<const f32x4*>(o + k * W::kRows * kMergeStride);
+      if ((on >> k) & 1u) sum += *reinterpret_cast<const f32x4*>(o + k * kRows * kMergeStride);
     return sum;
   }
   LVS_DEV float merged_max(int row) {
     const float* sm_m = reinterpret_cast<const float*>(smem);
     float mm = sm_m[row];
 #pragma unroll
-    for (int k = 1; k < KS; ++k) mm = fmaxf(mm, sm_m[k * W::kRows + row]);
+    for (int k = 1; k < KS; ++k) mm = fmaxf(mm, sm_m[k * kRows + row]);
     return mm;
   }
 
@@ -631,10 +741,10 @@ struct Segment {
 
 LVS_DEV float* record_at(const PagedAttnKernelArgs& p, int64_t i) { return p.ws + i * ((int64_t)p.rpad * 131); }
 
-template <int NB, int KS, bool ONCE>
+template <class Rows, int KS, bool ONCE>
 __global__ __launch_bounds__(64 * KS, 2) void paged_attn_kernel(PagedAttnKernelArgs p) {
   extern __shared__ __align__(256) uint8_t smem[];
-  Segment<NB, KS, ONCE> sg(p, smem);
+  Segment<Rows, KS, ONCE> sg(p, smem);
   const int HR = p.Hkv * p.n_rc, lane = threadIdx.x & 63;
   const int places0 = places_of(p, lane);
   const Cut cut = cut_units<KS>(p, lane, places0);
@@ -688,10 +798,10 @@ __global__ __launch_bounds__(64 * KS, 2) void paged_attn_kernel(PagedAttnKernelA
 }
 
 // One workgroup per unit, straight to the output: for tables so narrow that cutting a unit does not pay.
-template <int NB, int KS, bool ONCE>
+template <class Rows, int KS, bool ONCE>
 __global__ __launch_bounds__(64 * KS, 2) void paged_attn_unit_kernel(PagedAttnKernelArgs p) {
   extern __shared__ __align__(256) uint8_t smem[];
-  Segment<NB, KS, ONCE> sg(p, smem);
+  Segment<Rows, KS, ONCE> sg(p, smem);
   const int bh = (int)((uint32_t)blockIdx.x / (uint32_t)p.n_rc), rc = blockIdx.x - bh * p.n_rc;
   const int b = (int)((uint32_t)bh / (uint32_t)p.Hkv), h = bh - b * p.Hkv;
   const int L = paged_len(p.kv_len[b], p.cols);
@@ -818,16 +928,16 @@ int64_t unit_columns(int64_t units, int64_t cus) {
   return units >= cus ? 64 : units >= cus / 4 ? 32 : 20;
 }
 
-template <int NB, int KS, bool ONCE>
+template <class Rows, int KS, bool ONCE>
 hipError_t launch_line(const PagedAttnKernelArgs& a, hipStream_t stream) {
   static LdsLimitOnce limit;
-  constexpr size_t lds = Shape<NB, KS>::kLds;
-  hipError_t e = limit.ensure(reinterpret_cast<const void*>(&paged_attn_kernel<NB, KS, ONCE>), lds);
+  constexpr size_t lds = segment_lds<Rows, KS>();
+  hipError_t e = limit.ensure(reinterpret_cast<const void*>(&paged_attn_kernel<Rows, KS, ONCE>), lds);
   if (e != hipSuccess) return e;
   const unsigned units = (unsigned)(a.B * a.Hkv * a.n_rc);
   // (a part for every unit at least; the grid is a multiple of 8)
   const unsigned wgs = ((units > (unsigned)a.n_wg ? units : (unsigned)a.n_wg) + 7) / 8 * 8;
-  paged_attn_kernel<NB, KS, ONCE><<<dim3(wgs), dim3(64 * KS), lds, stream>>>(a);
+  paged_attn_kernel<Rows, KS, ONCE><<<dim3(wgs), dim3(64 * KS), lds, stream>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   // records of a unit, about: n_wg / units + 1
@@ -838,14 +948,14 @@ hipError_t launch_line(const PagedAttnKernelArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <int NB, int KS, bool ONCE>
+template <class Rows, int KS, bool ONCE>
 hipError_t launch_units(const PagedAttnKernelArgs& a, hipStream_t stream) {
   static LdsLimitOnce limit;
-  constexpr size_t lds = Shape<NB, KS>::kLds;
-  hipError_t e = limit.ensure(reinterpret_cast<const void*>(&paged_attn_unit_kernel<NB, KS, ONCE>), lds);
+  constexpr size_t lds = segment_lds<Rows, KS>();
+  hipError_t e = limit.ensure(reinterpret_cast<const void*>(&paged_attn_unit_kernel<Rows, KS, ONCE>), lds);
   if (e != hipSuccess) return e;
   const unsigned units = (unsigned)(a.B * a.Hkv * a.n_rc);
-  paged_attn_unit_kernel<NB, KS, ONCE><<<dim3(units), dim3(64 * KS), lds, stream>>>(a);
+  paged_attn_unit_kernel<Rows, KS, ONCE><<<dim3(units), dim3(64 * KS), lds, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -861,11 +971,11 @@ hipError_t launch_paged_attn(const PagedAttnKernelArgs& a, hipStream_t stream) {
   const bool once = a.n_rc == 1;
   const int64_t units = (int64_t)a.B * a.Hkv * a.n_rc, cus = a.n_wg / 2;
   if (a.cols <= unit_columns(units, cus)) {
-    if (a.rpad <= 16) return once ? launch_units<1, 8, true>(a, stream) : launch_units<1, 8, false>(a, stream);
-    return once ? launch_units<2, 8, true>(a, stream) : launch_units<2, 8, false>(a, stream);
+    if (a.rpad <= 16) return once ? launch_units<Rows16, 8, true>(a, stream) : launch_units<Rows16, 8, false>(a, stream);
+    return once ? launch_units<Rows32Core, 8, true>(a, stream) : launch_units<Rows32Core, 8, false>(a, stream);
   }
-  if (a.rpad <= 16) return once ? launch_line<1, 4, true>(a, stream) : launch_line<1, 4, false>(a, stream);
-  return once ? launch_line<2, 4, true>(a, stream) : launch_line<2, 4, false>(a, stream);
+  if (a.rpad <= 16) return once ? launch_line<Rows16, 4, true>(a, stream) : launch_line<Rows16, 4, false>(a, stream);
+  return once ? launch_line<Rows32Core, 4, true>(a, stream) : launch_line<Rows32Core, 4, false>(a, stream);
 }
 
 }  // namespace lvspec
