@@ -136,7 +136,7 @@ LVS_DEV Cut cut_units(const PagedAttnKernelArgs& p, int lane, int places0) {
   // Parts for one workgroup per CU (and some more of open rows only), or, where those take many rounds of
   // the streams, for two.
   c.len = 0;
-  int limit = max(cus, units) + min(units, cus >> 3), part = 0;
+  int limit = min(max(cus, units) + min(units, cus >> 3), p.n_wg), part = 0;
   for (int wide = 0; wide < 2; ++wide) {
     part = max((about(total, limit) + KS - 1) / KS * KS, kOpenTiles);
     while (true) {
@@ -692,21 +692,38 @@ struct Segment {
     if (lane < kRows) *reinterpret_cast<float2*>(o + 128) = float2{l, lv};
   }
 
-  // sums over the active streams of four floats of a row
-  LVS_DEV f32x4 merged(uint32_t on, int row, int c4) {
+  // Sums over the active streams of four floats of a row.  (All are read, at once: in the place of one that has
+  // nothing is whatever was there, and is not added.)
+  LVS_DEV f32x4 merged(uint32_t on, int row, int c4) const {
     const float* o = reinterpret_cast<const float*>(smem) + KS * kRows + row * kMergeStride + c4;
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    f32x4 x[KS], sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < KS; ++k) x[k] = *reinterpret_cast<const f32x4*>(o + k * kRows * kMergeStride);
 #pragma unroll
     for (int k = 0; k < KS; ++k)
-      if ((on >> k) & 1u) sum += *reinterpret_cast<const f32x4*>(o + k * kRows * kMergeStride);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[i] += (on >> k) & 1u ? x[k][i] : 0.f;
     return sum;
   }
-  LVS_DEV float merged_max(int row) {
+  LVS_DEV float merged_max(int row) const {
     const float* sm_m = reinterpret_cast<const float*>(smem);
     float mm = sm_m[row];
 #pragma unroll
     for (int k = 1; k < KS; ++k) mm = fmaxf(mm, sm_m[k * kRows + row]);
     return mm;
+  }
+  // denominator and its share on the video span, by the 32 lanes that have the row
+  LVS_DEV float2 merged_sums(uint32_t on, int row, int l32) const {
+    const float* o = reinterpret_cast<const float*>(smem) + KS * kRows + row * kMergeStride + 128;
+    const int k = l32 & (KS - 1);
+    float2 x = *reinterpret_cast<const float2*>(o + k * kRows * kMergeStride);
+    x = (on >> k) & 1u ? x : float2{0.f, 0.f};
+#pragma unroll
+    for (int d = 1; d < KS; d <<= 1) {
+      x.x += xor_shuffle(x.x, d);
+      x.y += xor_shuffle(x.y, d);
+    }
+    return x;
   }
 
   // the merged state into a record
@@ -716,13 +733,13 @@ struct Segment {
     const int rows = min(p.R - rc * p.rpad, p.rpad);
     for (int idx = threadIdx.x; idx < rows * 32; idx += 64 * KS) {
       const int row = idx >> 5, l32 = idx & 31;
+      const float2 l = merged_sums(on, row, l32);
       *reinterpret_cast<f32x4*>(rec + 3 * p.rpad + row * 128 + l32 * 4) = merged(on, row, l32 * 4);
-    }
-    for (int row = threadIdx.x; row < rows; row += 64 * KS) {
-      const f32x4 l = merged(on, row, 128);
-      rec[row] = merged_max(row);
-      rec[p.rpad + row] = l[0];
-      rec[2 * p.rpad + row] = l[1];
+      if (l32 == 0) {
+        rec[row] = merged_max(row);
+        rec[p.rpad + row] = l.x;
+        rec[2 * p.rpad + row] = l.y;
+      }
     }
   }
 
@@ -733,8 +750,9 @@ struct Segment {
     const int rows = min(p.R - rc * p.rpad, p.rpad);
     for (int idx = threadIdx.x; idx < rows * 32; idx += 64 * KS) {
       const int row = idx >> 5, l32 = idx & 31;
-      const f32x4 l = merged(on, row, 128);
-      write_row(p, b, h, rc * p.rpad + row, l32, merged(on, row, l32 * 4), merged_max(row), l[0], l[1]);
+      const float2 l = merged_sums(on, row, l32);
+      const float mm = p.lse != nullptr ? merged_max(row) : 0.f;
+      write_row(p, b, h, rc * p.rpad + row, l32, merged(on, row, l32 * 4), mm, l.x, l.y);
     }
   }
 };
@@ -928,6 +946,7 @@ int64_t unit_columns(int64_t units, int64_t cus) {
   return units >= cus ? 64 : units >= cus / 4 ? 32 : 20;
 }
 
+// fewer units than n_wg: a part for each at least
 template <class Rows, int KS, bool ONCE>
 hipError_t launch_line(const PagedAttnKernelArgs& a, hipStream_t stream) {
   static LdsLimitOnce limit;
@@ -935,9 +954,7 @@ hipError_t launch_line(const PagedAttnKernelArgs& a, hipStream_t stream) {
   hipError_t e = limit.ensure(reinterpret_cast<const void*>(&paged_attn_kernel<Rows, KS, ONCE>), lds);
   if (e != hipSuccess) return e;
   const unsigned units = (unsigned)(a.B * a.Hkv * a.n_rc);
-  // (a part for every unit at least; the grid is a multiple of 8)
-  const unsigned wgs = ((units > (unsigned)a.n_wg ? units : (unsigned)a.n_wg) + 7) / 8 * 8;
-  paged_attn_kernel<Rows, KS, ONCE><<<dim3(wgs), dim3(64 * KS), lds, stream>>>(a);
+  paged_attn_kernel<Rows, KS, ONCE><<<dim3((unsigned)a.n_wg), dim3(64 * KS), lds, stream>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   // records of a unit, about: n_wg / units + 1

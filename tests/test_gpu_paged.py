@@ -248,6 +248,9 @@ ATTNS = [
     dict(kv=[(37 * i) % 700 for i in range(70)], g=1, Hq=4, Hkv=2),                         # more than a wave of sequences
     dict(kv=[9000], g=3, Hq=3, Hkv=1), dict(kv=[6000, 10, 3000], g=16, Hq=4, Hkv=4),
     dict(kv=[800], g=2, Hq=64, Hkv=2), dict(kv=[450], g=33 // 3, Hq=3, Hkv=1, scale=0.3),
+    # nearly as many units as workgroups, some of them long: parts, or one line; then more units than workgroups
+    dict(kv=[1200, 300] + [17] * 60, g=1, Hq=8, Hkv=8), dict(kv=[9600] * 10 + [20] * 50, g=1, Hq=8, Hkv=8),
+    dict(kv=[25000, 24000, 26000], g=1, Hq=16, Hkv=16), dict(kv=[(53 * i) % 300 for i in range(70)], g=2, Hq=8, Hkv=8),
 ]
 
 
@@ -324,12 +327,14 @@ def test_attention_masked_draft_rows_do_not_reach_others(L, value, spare_cols):
     assert torch.equal(got[:, :3], want[:, :3])
 
 
-def test_attention_lengths_and_blocks_out_of_range(L):
+@pytest.mark.parametrize("spare_cols", [0, 50])
+def test_attention_lengths_and_blocks_out_of_range(L, spare_cols):
     """Lengths are clamped to what the table names; entries that name no block hold no key."""
     kv, g = [300, 300, 300], 3
-    cache, table = ready(L, 96, 3, 2, kv, spare_cols=0)
+    cache, table = ready(L, 96, 3, 2, kv, spare_cols=spare_cols)
     q = normal(97, (3, g, 4, D))
     table[1, 2], table[2, 0] = -1, cache.k_pool.shape[0]
+    assert table.shape[1] == 4 + spare_cols
     check_attention(L, q, cache, table, kv)
     most = table.shape[1] * T + T - 1
     a = L.verify_attn_paged(q, cache, i32(table), i32([-5, 10 ** 9, most]))
