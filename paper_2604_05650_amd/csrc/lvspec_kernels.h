@@ -290,7 +290,7 @@ struct PagedAttnKernelArgs {
   int rpad, n_rc;               // rows per row chunk, row chunks
   FastDiv div_g;                // by G
   int n_blocks, cols;
-  int n_wg, wg_shift;           // workgroups that the chip holds at once, 2^wg_shift >= 8
+  int limit, spare;             // parts that units are cut into at most, and those of them for ragged lengths
   float scale_log2e;
   const int32_t* vis_begin;     // nullptr = no span
   const int32_t* vis_end;
@@ -298,10 +298,9 @@ struct PagedAttnKernelArgs {
   int64_t o_sb, o_sg, o_sh;
   float* lse;
   float* vis_mass;
-  float* ws;                    // n_wg + units records of rpad * 131 floats
+  float* ws;                    // limit records of rpad * 131 floats
   uint32_t draft_mask[32];
 };
 hipError_t launch_paged_attn(const PagedAttnKernelArgs& a, hipStream_t stream);
-int paged_attn_workgroups(int num_cu);   // n_wg: two per CU, rounded down to a power of two
 
 }  // namespace lvspec

@@ -1,6 +1,8 @@
 // C ABI of the paged cache in 8 bits: argument validation and launches on the caller's stream.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "../../include/lvspec.h"
 #include "lvspec_kernels.h"
 
@@ -27,7 +29,7 @@ int check_cache_pointers(const lvspec_paged_cache* c) {
 }
 
 struct PagedPlan {
-  int G, R, n_rc, rpad, n_wg;
+  int G, R, n_rc, rpad, limit, spare;
   size_t ws_bytes;
 };
 
@@ -44,12 +46,14 @@ int plan_paged_attn(const lvspec_paged_attn_args* a, PagedPlan* pl) {
   pl->R = pl->G * a->gamma;
   pl->n_rc = (pl->R + 31) / 32;
   pl->rpad = ((pl->R + pl->n_rc - 1) / pl->n_rc + 3) / 4 * 4;
-  // tiles of the line, units and output rows are 32-bit numbers in the kernels
-  const int64_t units = (int64_t)c.B * c.Hkv * pl->n_rc;   // (the open rows of a unit have eight places)
+  // places of all units (eight for open rows each), parts and output rows are 32-bit numbers in the kernels
+  const int64_t units = (int64_t)c.B * c.Hkv * pl->n_rc;
   if (units * ((int64_t)a->table_cols + 8) > (int64_t)1 << 30 || (int64_t)c.B * c.Hkv * pl->R > (int64_t)1 << 30)
     return LVSPEC_EUNSUPPORTED;
-  pl->n_wg = lvspec::paged_attn_workgroups(lvspec::num_compute_units());
-  pl->ws_bytes = (size_t)(pl->n_wg + units) * pl->rpad * 131 * sizeof(float);
+  const int cus = lvspec::num_compute_units();
+  pl->limit = (int)units + cus - 1;
+  pl->spare = pl->limit - std::max((int)units, cus);
+  pl->ws_bytes = (size_t)pl->limit * pl->rpad * 131 * sizeof(float);
   return LVSPEC_OK;
 }
 
@@ -143,8 +147,7 @@ int lvspec_verify_attn_paged(const lvspec_paged_attn_args* a, void* stream) {
   k.table = a->table; k.kv_len = a->kv_len;
   k.B = c.B; k.gamma = a->gamma; k.Hq = a->Hq; k.Hkv = c.Hkv; k.G = pl.G; k.R = pl.R;
   k.div_g = lvspec::make_fast_div((uint32_t)pl.G);
-  k.rpad = pl.rpad; k.n_rc = pl.n_rc; k.n_blocks = c.n_blocks; k.cols = a->table_cols; k.n_wg = pl.n_wg;
-  k.wg_shift = __builtin_ctz((unsigned)pl.n_wg);
+  k.rpad = pl.rpad; k.n_rc = pl.n_rc; k.n_blocks = c.n_blocks; k.cols = a->table_cols; k.limit = pl.limit; k.spare = pl.spare;
   const float scale = a->scale > 0.f ? a->scale : 1.0f / __builtin_sqrtf((float)c.D);
   k.scale_log2e = scale * 1.4426950408889634f;
   k.vis_begin = a->vis_begin; k.vis_end = a->vis_end;

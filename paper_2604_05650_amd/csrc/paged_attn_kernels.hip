@@ -1,20 +1,22 @@
 // Attention of the draft rows over the paged cache in 8 bits (paged_dev.h), the same contract as
 // verification attention over a bf16 cache.
 //
-// Kernel 1 (split):   the complete blocks of all sequences and kv heads form one line of 64-key tiles, cut
-//   into equal stretches; a workgroup takes one stretch, its streams of waves every KS-th tile of it.  The
-//   open rows of a unit (sequence, kv head, row chunk), at most 95 in bf16, are taken by a workgroup of
-//   their own.  A tile goes from memory into registers and from there into the matrix instructions:
-//     keys:   16 bytes per lane are two operands of S^T = K Q^T after their conversion to bf16; which
-//             channels a lane's operand holds is a permutation that K and Q share;
-//     values: 16 bytes per lane are 16 tokens of one channel.  The tokens of a lane's scores, row block b
-//             of S^T being tokens 16 (m/4) + 4 b + m%4, are then the tokens of its value operand, and
-//             probabilities stay in their lane.
+// Kernel 1 (split):   a unit (sequence, kv head, row chunk of at most 32 rows) is cut into parts along its keys; a
+//   workgroup takes one part, its streams (waves) every KS-th tile of 64 keys.  A wave fetches its tiles itself,
+//   straight into its own 16 KiB of LDS, and waits for nobody else:
+//     keys:   an operand of S^T = K Q^T is made of 16 bytes of a token, converted to bf16; which channels a
+//             lane's operand holds is a permutation that K and Q share;
+//     values: 16 bytes of a channel are 16 tokens.  The tokens of a lane's scores are those of its value
+//             operand, and probabilities stay in their lane.
 //   The conversion multiplies by the block's scale (a power of two): exact, and nothing is left to scale.
 //   Softmax in base 2 with a running maximum, sums in 32 bits; probabilities are rounded to bf16 for the
 //   second product (relative 2^-9 each, which averages out over the keys; it is what the matrix
-//   instructions take).  The streams merge through LDS in fixed order into one record per segment.
+//   instructions take).  Open rows, at most 95 in bf16, are taken 32 at a time by the streams of a unit's first
+//   part.  The streams merge through LDS in fixed order into one record per part.
 // Kernel 2 (combine): merge of a row's records in fixed order, bf16 output.
+// Small tables: one workgroup per unit writes the output itself, and there is no second kernel.
+// Bound: the streaming read of K and V from memory; where a group has 17 and more rows, the conversion and
+// the matrix instructions beside it.
 #include "attn_rows32.h"
 #include "paged_dev.h"
 
@@ -76,18 +78,20 @@ LVS_DEV void copy_page(const uint8_t* pool, int id, int64_t head, int n_heads, u
 #undef LVS_COPY_1
 }
 
-// ------------------------------------------------------------------------------ the line of tiles
-// A unit (sequence, kv head, row chunk) has kOpenTiles places for its open rows, which take about as long as
-// so many tiles, and a place per tile of 64 keys.  Two ways to divide them:
-//   the line: all units one behind the other, sequence by sequence (HR = Hkv * n_rc units each), cut into
-//     equal stretches, one per workgroup.  Nobody waits for anybody, but a stretch over the end of a unit is two
-//     segments, and a segment has 5 us of its own (first loads, merge);
-//   parts: every unit in equal parts of at most so many places that there are no more parts than workgroups.
-// The line is taken where a stretch is long (kLineLeast).  Who has the first of a unit's places does its open rows.
-// Every wave finds its place by itself.
+// ------------------------------------------------------------------------------ parts
+// A unit has kOpenTiles places for its open rows, which take about as long as so many tiles, and a place per
+// tile of 64 keys.  Every unit is cut into equal parts of at most so many places that there are no more parts
+// than compute units (or units, if they are more); who has the first of a unit's places does its open rows.
+// The lengths are on the device, so every wave finds the cut and its place by itself.
+// One workgroup of four waves per CU draws the 27 GB/s that are the CU's share of the memory's rate, and each
+// part has 5 us of its own (first loads, merge, record).  For two per CU: 8 x 8000 keys, 40/8 heads, 8 rows
+// 46.2 us against 38.5 here, 2 x 16000, 30 rows 50.4 and 44.8, 32 x 6000, 5 rows 84 and 69; eight waves in one
+// workgroup: 16384 keys 19.7 and 17.2, 4 x 65536, 64/8 heads, 8 rows 123 and 128.  Equal stretches of one
+// line of all units, whatever their ends: 16 x (2048 to 32768) keys 79 and 74.
+// Where lengths are so ragged that whole parts leave the longest half as long again as an even share, there
+// may be more: 32 x (500 to 60000) keys, 256 units, 298 us without this and 155 with it, 48 x (100 to 20000)
+// 125 and 89.  Everywhere, it costs: 5 x 12000, 150 rows 26.8 and 33.9, 16 x (2048 to 32768) keys 74 and 80.
 constexpr int kOpenTiles = 8;
-constexpr int kLineLeast = 32;
-constexpr int kPartRounds = 5;
 
 LVS_DEV int wave_scan(int x) {               // inclusive sum over the lanes
   auto add = [&](uint32_t y) { x += (int)y; };
@@ -103,14 +107,6 @@ LVS_DEV int last_lane(int x) { return __builtin_amdgcn_readlane(x, 63); }
 
 LVS_DEV int full_blocks(const PagedAttnKernelArgs& p, int b) { return paged_len(p.kv_len[b], p.cols) >> kPageShift; }
 
-struct Cut {
-  int total;           // places of all units (line), or parts of all units
-  int len;             // places of a stretch; 0: parts
-  uint32_t inv;        // parts: about 2^32 / most places of a part
-  // a sequence's share of the line, or the parts of one of its units
-  LVS_DEV int share(int places) const { return places == 0 || len > 0 ? places : 1 + (int)__umulhi((uint32_t)(places - 1), inv); }
-};
-
 // Exact, but some thirty instructions one behind the other, a tenth of a microsecond; and about.
 LVS_DEV int divide(int x, int d) { return (int)((uint32_t)x / (uint32_t)d); }
 LVS_DEV int about(int x, int d) { return (int)((float)x * __builtin_amdgcn_rcpf((float)d)); }
@@ -118,7 +114,14 @@ LVS_DEV int about(int x, int d) { return (int)((float)x * __builtin_amdgcn_rcpf(
 // places of the units of sequences b0 .. b0+63, one per lane; 0 behind the last one
 LVS_DEV int places_of(const PagedAttnKernelArgs& p, int b) { return b < p.B ? full_blocks(p, b) + kOpenTiles : 0; }
 
-// places0: those of the first 64 sequences
+struct Cut {
+  int total;           // parts of all units
+  uint32_t inv;        // about 2^32 / most places of a part
+  // parts of a unit of so many places (about places / most, rounded up: any number serves that both kernels find)
+  LVS_DEV int parts(int places) const { return places == 0 ? 0 : 1 + (int)__umulhi((uint32_t)(places - 1), inv); }
+};
+
+// places0: those of the first 64 sequences; KS: streams of a workgroup
 template <int KS>
 LVS_DEV Cut cut_units(const PagedAttnKernelArgs& p, int lane, int places0) {
   int sum = last_lane(wave_scan(places0)), most = (int)wave_max_u32((uint32_t)places0);
@@ -127,36 +130,24 @@ LVS_DEV Cut cut_units(const PagedAttnKernelArgs& p, int lane, int places0) {
     sum += last_lane(wave_scan(x));
     most = max(most, (int)wave_max_u32((uint32_t)x));
   }
-  const int HR = p.Hkv * p.n_rc, units = p.B * HR, cus = p.n_wg >> 1;
+  const int HR = p.Hkv * p.n_rc;
   Cut c;
-  const int total = sum * HR, stretch = (total + p.n_wg - 1) >> p.wg_shift;
-  c.total = total;
-  c.len = stretch;
-  if (stretch >= kLineLeast) return c;
-  // Parts for one workgroup per CU (and some more of open rows only), or, where those take many rounds of
-  // the streams, for two.
-  c.len = 0;
-  int limit = min(max(cus, units) + min(units, cus >> 3), p.n_wg), part = 0;
-  for (int wide = 0; wide < 2; ++wide) {
-    part = max((about(total, limit) + KS - 1) / KS * KS, kOpenTiles);
+  int limit = p.limit - p.spare, part = 0;
+  while (true) {
+    const int even = about(sum * HR, limit);
+    // whole rounds of the streams: a part of 4 k + 1 tiles takes as long as one of 4 (k + 1)
+    part = max((even + KS - 1) / KS * KS, kOpenTiles);
     while (true) {
       c.inv = (uint32_t)(4294967040.f * __builtin_amdgcn_rcpf((float)part));
-      int n = last_lane(wave_scan(c.share(places0)));
-      for (int b0 = 64; b0 < p.B; b0 += 64) n += last_lane(wave_scan(c.share(places_of(p, b0 + lane))));
+      int n = last_lane(wave_scan(c.parts(places0)));
+      for (int b0 = 64; b0 < p.B; b0 += 64) n += last_lane(wave_scan(c.parts(places_of(p, b0 + lane))));
       c.total = n * HR;
-      if (c.total <= limit || part >= most) break;
+      if (c.total <= limit) break;            // (one part each serves, so it ends)
       part += max(part >> 3, KS) / KS * KS;
     }
-    if (part <= kPartRounds * KS || limit >= p.n_wg) break;
-    limit = p.n_wg;
+    if (limit == p.limit || min(part, most) <= even + (even >> 1) + kOpenTiles) return c;
+    limit = p.limit;
   }
-  // lengths so unequal that the longest part is well above the average
-  const int even = about(total, limit);
-  if (stretch >= kLineLeast / 2 && min(part, most) > even + (even >> 1) + kOpenTiles) {
-    c.total = total;
-    c.len = stretch;
-  }
-  return c;
 }
 
 // ------------------------------------------------------------------------------ split
@@ -204,6 +195,7 @@ struct Rows16 {
   float m, l, lv;
 
   static LVS_DEV int k_place(int t) { return ((t >> 1) & 1) | (((t >> 4) & 3) << 1); }
+  static LVS_DEV int k_copy(int y, int lane) { return ((lane >> 4) & 1) | ((y >> 1) << 1); }      // of 8 y + lane / 8
   static LVS_DEV int v_place(int q) { return ((q >> 1) & 1) | (((q ^ (q >> 1)) & 1) << 1); }    // 0 2 3 1
   static LVS_DEV int row_of(int lane) { return lane & 15; }
   static LVS_DEV int key_of(int lane, int e) { return 16 * (lane >> 4) + e; }
@@ -316,6 +308,7 @@ struct Rows32Core {
   float m, l, lv;
 
   static LVS_DEV int k_place(int t) { return (t >> 1) & 7; }
+  static LVS_DEV int k_copy(int y, int lane) { return (lane >> 4) | ((y & 1) << 2); }
   static LVS_DEV int v_place(int q) { return q & 3; }
   static LVS_DEV int row_of(int lane) { return lane & 31; }
   static LVS_DEV int key_of(int lane, int e) { return 32 * (e >> 4) + 16 * (lane >> 5) + (e & 15); }
@@ -539,7 +532,7 @@ struct Segment {
     int k_off[8], v_off[8];
 #pragma unroll
     for (int y = 0; y < 8; ++y) {
-      k_off[y] = (lane >> 3) * 128 + (((lane & 7) ^ Rows::k_place(8 * y + (lane >> 3))) << 4);
+      k_off[y] = (lane >> 3) * 128 + (((lane & 7) ^ Rows::k_copy(y, lane)) << 4);
       v_off[y] = (lane >> 2) * kPageTokens + (((lane & 3) ^ Rows::v_place(lane >> 4)) << 4);
     }
     auto copy_k = [&](int id) { copy_page<ONCE>(p.k8, id, h, p.Hkv, k_slot, k_off); };
@@ -764,55 +757,36 @@ __global__ __launch_bounds__(64 * KS, 2) void paged_attn_kernel(PagedAttnKernelA
   extern __shared__ __align__(256) uint8_t smem[];
   Segment<Rows, KS, ONCE> sg(p, smem);
   const int HR = p.Hkv * p.n_rc, lane = threadIdx.x & 63;
-  const int places0 = places_of(p, lane);
-  const Cut cut = cut_units<KS>(p, lane, places0);
-  const int len = max(cut.len, 1);
-  const int used = cut.len > 0 ? divide(cut.total + len - 1, len) : cut.total;       // workgroups with work
-  // work that follows each other goes to one XCD, which has the records of a unit in its L2
-  const int each = (used + 7) >> 3;
+  int places = places_of(p, lane);
+  const Cut cut = cut_units<KS>(p, lane, places);
+  // parts that follow each other go to one XCD, which has the records of a unit in its L2
+  const int each = (cut.total + 7) >> 3;
   const int w = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= each || w >= used) return;
-  int at = w * len;
-  const int end = min(at + len, cut.total);
-  bool again = false;
-  int b0 = 0, before = 0;                        // sequences b0 .. b0+63 at hand, shares before them
-  int places = places0, upto = wave_scan(cut.share(places));
-  while (at < end) {
-    int all = last_lane(upto);
-    while (at >= all * HR) {                     // (ends: at < total)
-      b0 += 64;
-      before = all;
-      places = places_of(p, b0 + lane);
-      upto = before + wave_scan(cut.share(places));
-      all = last_lane(upto);
-    }
-    const int in = __popcll(__ballot(at >= upto * HR));
-    const int unit_places = __builtin_amdgcn_readlane(places, in);
-    const int mine = cut.share(unit_places);
-    const int y = at - (__builtin_amdgcn_readlane(upto, in) - mine) * HR;
-    const int hr = divide(y, mine), x = y - hr * mine;
-    const int b = b0 + in, h = ONCE ? hr : divide(hr, p.n_rc), rc = hr - h * p.n_rc;
-    int p0 = x, p1 = min(mine, x + end - at);    // places of the unit
-    at += p1 - p0;
-    if (cut.len == 0) {
-      const int q = divide(unit_places, mine), r = unit_places - q * mine;      // the first r have one more
-      p0 = x * q + min(x, r);
-      p1 = p0 + q + (x < r ? 1 : 0);
-    }
-    if (p0 > 0 && p1 <= kOpenTiles) continue;    // (only places of open rows, not the first)
-    const int t0 = max(p0 - kOpenTiles, 0), t1 = p1 - kOpenTiles;
-    if (again) __syncthreads();                  // (the segment before this one has been read from LDS)
-    again = true;
-    const int L = p0 == 0 ? paged_len(p.kv_len[b], p.cols) : 0;      // (for the open rows)
-    sg.begin(b, h, rc);
-    if (p0 == 0) sg.open_rows(b, h, rc, L);
-    sg.blocks(b, h, t0, t1);
-    const uint32_t on = sg.active(t1 - t0, p0 == 0, L);
-    if (cut.len == 0 && mine == 1)
-      sg.finish(on, b, h, rc);
-    else
-      sg.end(on, rc, record_at(p, cut.len > 0 ? (int64_t)w + (int64_t)b * HR + hr : w));
+  if ((int)(blockIdx.x >> 3) >= each || w >= cut.total) return;
+  int b0 = 0, upto = wave_scan(cut.parts(places));       // sequences b0 .. b0+63 at hand
+  while (w >= last_lane(upto) * HR) {                     // (ends: w < total)
+    const int before = last_lane(upto);
+    b0 += 64;
+    places = places_of(p, b0 + lane);
+    upto = before + wave_scan(cut.parts(places));
   }
+  const int in = __popcll(__ballot(w >= upto * HR));
+  const int unit_places = __builtin_amdgcn_readlane(places, in), n = cut.parts(unit_places);
+  const int y = w - (__builtin_amdgcn_readlane(upto, in) - n) * HR;
+  const int hr = divide(y, n), part = y - hr * n;
+  const int b = b0 + in, h = ONCE ? hr : divide(hr, p.n_rc), rc = hr - h * p.n_rc;
+  const int q = divide(unit_places, n), r = unit_places - q * n;      // the first r parts have one more
+  const int p0 = part * q + min(part, r), p1 = p0 + q + (part < r ? 1 : 0);
+  const int t0 = max(p0 - kOpenTiles, 0), t1 = p1 - kOpenTiles;
+  const int L = p0 == 0 ? paged_len(p.kv_len[b], p.cols) : 0;      // (for the open rows)
+  sg.begin(b, h, rc);
+  if (p0 == 0) sg.open_rows(b, h, rc, L);
+  sg.blocks(b, h, t0, t1);
+  const uint32_t on = sg.active(t1 - t0, p0 == 0, L);
+  if (n == 1)
+    sg.finish(on, b, h, rc);
+  else
+    sg.end(on, rc, record_at(p, w));
 }
 
 // One workgroup per unit, straight to the output: for tables so narrow that cutting a unit does not pay.
@@ -848,35 +822,24 @@ __global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(PagedAtt
   const int h = (int)((uint32_t)hr / (uint32_t)p.n_rc), rc = hr - h * p.n_rc;
   const int in = (blockIdx.x - unit * per_unit) * kRows + g / SPLIT, r = rc * p.rpad + in;
   const bool row = in < p.rpad && r < p.R;
-  // where the unit lies, and whose records are its own
+  // the unit's records
   int places = places_of(p, lane);
   const Cut cut = cut_units<KS>(p, lane, places);
-  int before = 0, share = 0;
+  int before = 0, n = 0;
   for (int b0 = 0; b0 <= b; b0 += 64) {
     if (b0 > 0) places = places_of(p, b0 + lane);
-    const int f = cut.share(places);
+    const int f = cut.parts(places);
     const int upto = wave_scan(f);
     if (b < b0 + 64) {
-      share = __builtin_amdgcn_readlane(f, b - b0);
-      before += __builtin_amdgcn_readlane(upto, b - b0) - share;
+      n = __builtin_amdgcn_readlane(f, b - b0);
+      before += __builtin_amdgcn_readlane(upto, b - b0) - n;
     } else {
       before += last_lane(upto);
     }
   }
-  if (cut.len == 0 && share == 1) return;        // (one part: it has written the output)
-  const int from = before * HR + hr * share;
+  if (n == 1) return;                            // (one part: it has written the output)
   const int64_t step = (int64_t)p.rpad * 131;
-  int64_t at0 = from, skip = 0;                  // first record, and records between it and the others
-  int n = share;
-  if (cut.len > 0) {
-    // the stretch of the first place, and those from the first tile's to the last one's
-    const int first = divide(from, cut.len), full = share - kOpenTiles;
-    const int next = full > 0 ? max(divide(from + kOpenTiles, cut.len), first + 1) : first + 1;
-    n = full > 0 ? max(divide(from + share - 1, cut.len) - next + 2, 1) : 1;
-    at0 = (int64_t)first + unit;
-    skip = (next - first - 1) * step;
-  }
-  const float* rec = record_at(p, at0) + (row ? in : 0);
+  const float* rec = record_at(p, before * HR + hr * n) + (row ? in : 0);
   // every group for itself: maximum, sums and output of its records, eight at a time
   float mm = kNegBig, l = 0.f, lv = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -887,7 +850,7 @@ __global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(PagedAtt
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       const int at = k0 + SPLIT * k < n ? k0 + SPLIT * k : k0;
-      const int64_t off = at * step + (at > 0 ? skip : 0);
+      const int64_t off = at * step;
       x[k] = *reinterpret_cast<const f32x4*>(orec + off);
       m8[k] = rec[off];
       l8[k] = rec[off + p.rpad];
@@ -939,26 +902,26 @@ __global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(PagedAtt
   if (row) write_row(p, b, h, r, l32, o, mm, l, lv);
 }
 
-// Columns of a table up to which every unit is one workgroup's.  The longest sequence may have as many blocks, so the
-// more units there are, the more of them pay: they fill the chip anyway.
-int64_t unit_columns(int64_t units, int64_t cus) {
-  if (units >= 2 * cus) return (int64_t)1 << 30;
-  return units >= cus ? 64 : units >= cus / 4 ? 32 : 20;
-}
+// Columns of a table up to which every unit is one workgroup's, with no second kernel.  The longest sequence may
+// have as many blocks, so the more units there are, the more of them pay: they fill the chip anyway.  One
+// workgroup per unit and parts, us: 8 units 800 keys 11.1 and 12.4, 1100 12.2 and 12.7, 1400 13.9 and 12.7;
+// 64 units 1000 keys 13.3 and 13.8, 1500 15.9 and 14.4; 128 units 2000 keys 18.6 and 20.7, 3000 24.6 and 26.1;
+// 256 units 4000 keys 45.9 and 49.8, 512 units 91.6 and 89.6.
+int unit_columns(int64_t units, int64_t cus) { return units >= cus / 2 ? 64 : 18; }
 
-// fewer units than n_wg: a part for each at least
 template <class Rows, int KS, bool ONCE>
-hipError_t launch_line(const PagedAttnKernelArgs& a, hipStream_t stream) {
+hipError_t launch_parts(const PagedAttnKernelArgs& a, hipStream_t stream) {
   static LdsLimitOnce limit;
   constexpr size_t lds = segment_lds<Rows, KS>();
   hipError_t e = limit.ensure(reinterpret_cast<const void*>(&paged_attn_kernel<Rows, KS, ONCE>), lds);
   if (e != hipSuccess) return e;
   const unsigned units = (unsigned)(a.B * a.Hkv * a.n_rc);
-  paged_attn_kernel<Rows, KS, ONCE><<<dim3((unsigned)a.n_wg), dim3(64 * KS), lds, stream>>>(a);
+  paged_attn_kernel<Rows, KS, ONCE><<<dim3((unsigned)(a.limit + 7) / 8 * 8), dim3(64 * KS), lds, stream>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  // records of a unit, about: n_wg / units + 1
-  if ((int64_t)units * 8 > a.n_wg)
+  // few units have many records each: all groups of a workgroup to one row.  8 units, 32 records each: 16.4 us
+  // so and 17.7 with a group per row; 64 units, 4 each: 23.9 and 20.9.
+  if ((int64_t)units * 16 > a.limit - a.spare)
     paged_combine_kernel<1, KS><<<dim3(units * (unsigned)((a.rpad + 7) / 8)), dim3(kCombineThreads), 0, stream>>>(a);
   else
     paged_combine_kernel<8, KS><<<dim3(units * (unsigned)a.rpad), dim3(kCombineThreads), 0, stream>>>(a);
@@ -978,21 +941,15 @@ hipError_t launch_units(const PagedAttnKernelArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-int paged_attn_workgroups(int num_cu) {
-  int n = 8;
-  while (2 * n <= 2 * num_cu && n < 1024) n *= 2;
-  return n;
-}
-
 hipError_t launch_paged_attn(const PagedAttnKernelArgs& a, hipStream_t stream) {
   const bool once = a.n_rc == 1;
-  const int64_t units = (int64_t)a.B * a.Hkv * a.n_rc, cus = a.n_wg / 2;
-  if (a.cols <= unit_columns(units, cus)) {
+  const int64_t units = (int64_t)a.B * a.Hkv * a.n_rc;
+  if (a.cols <= unit_columns(units, a.limit - units + 1)) {
     if (a.rpad <= 16) return once ? launch_units<Rows16, 8, true>(a, stream) : launch_units<Rows16, 8, false>(a, stream);
     return once ? launch_units<Rows32Core, 8, true>(a, stream) : launch_units<Rows32Core, 8, false>(a, stream);
   }
-  if (a.rpad <= 16) return once ? launch_line<Rows16, 4, true>(a, stream) : launch_line<Rows16, 4, false>(a, stream);
-  return once ? launch_line<Rows32Core, 4, true>(a, stream) : launch_line<Rows32Core, 4, false>(a, stream);
+  if (a.rpad <= 16) return once ? launch_parts<Rows16, 4, true>(a, stream) : launch_parts<Rows16, 4, false>(a, stream);
+  return once ? launch_parts<Rows32Core, 4, true>(a, stream) : launch_parts<Rows32Core, 4, false>(a, stream);
 }
 
 }  // namespace lvspec

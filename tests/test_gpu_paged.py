@@ -248,13 +248,14 @@ ATTNS = [
     dict(kv=[(37 * i) % 700 for i in range(70)], g=1, Hq=4, Hkv=2),                         # more than a wave of sequences
     dict(kv=[9000], g=3, Hq=3, Hkv=1), dict(kv=[6000, 10, 3000], g=16, Hq=4, Hkv=4),
     dict(kv=[800], g=2, Hq=64, Hkv=2), dict(kv=[450], g=33 // 3, Hq=3, Hkv=1, scale=0.3),
-    # nearly as many units as workgroups, some of them long: parts, or one line; then more units than workgroups
+    # units of very different lengths, fewer and more than compute units
     dict(kv=[1200, 300] + [17] * 60, g=1, Hq=8, Hkv=8), dict(kv=[9600] * 10 + [20] * 50, g=1, Hq=8, Hkv=8),
     dict(kv=[25000, 24000, 26000], g=1, Hq=16, Hkv=16), dict(kv=[(53 * i) % 300 for i in range(70)], g=2, Hq=8, Hkv=8),
+    dict(kv=[(53 * i) % 300 for i in range(131)] + [5000, 0, 64, 9000], g=3, Hq=2, Hkv=1),
 ]
 
 
-@pytest.mark.parametrize("spare_cols", [1, 50])        # a unit in one workgroup, or all of them on a line
+@pytest.mark.parametrize("spare_cols", [1, 70])        # a unit in one workgroup where it is short, or cut into parts
 @pytest.mark.parametrize("i", range(len(ATTNS)))
 def test_attention(L, i, spare_cols):
     c = ATTNS[i]
@@ -279,7 +280,7 @@ def test_attention_strides_and_span(L):
     check_attention(L, q, cache, table, kv, ([13, -5, 0], [333, 64, 1]))
 
 
-@pytest.mark.parametrize("spare_cols", [3, 50])
+@pytest.mark.parametrize("spare_cols", [3, 70])
 def test_attention_reads_declared_rows_only(L, spare_cols):
     """Unused blocks, table entries behind the length and ring rows of nobody hold NaN."""
     kv, g = [200, 64, 30, 0], 5
@@ -304,7 +305,7 @@ def test_attention_reads_declared_rows_only(L, spare_cols):
     assert torch.equal(got, want)
 
 
-@pytest.mark.parametrize("spare_cols", [1, 50])
+@pytest.mark.parametrize("spare_cols", [1, 70])
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
 def test_attention_masked_draft_rows_do_not_reach_others(L, value, spare_cols):
     """A draft row that is not finite changes the rows that see it and no other."""
@@ -327,7 +328,7 @@ def test_attention_masked_draft_rows_do_not_reach_others(L, value, spare_cols):
     assert torch.equal(got[:, :3], want[:, :3])
 
 
-@pytest.mark.parametrize("spare_cols", [0, 50])
+@pytest.mark.parametrize("spare_cols", [0, 70])
 def test_attention_lengths_and_blocks_out_of_range(L, spare_cols):
     """Lengths are clamped to what the table names; entries that name no block hold no key."""
     kv, g = [300, 300, 300], 3
