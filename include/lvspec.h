@@ -426,7 +426,8 @@ int lvspec_paged_append(const lvspec_paged_append_args* args, void* stream);
  * table entry below L / 64 that names no block of the pool holds no key: its positions are left out.
  * Where a sequence's keys are cut, and with that the rounding of its bf16 probabilities (a relative 2e-3
  * of the result), follows from the lengths of all sequences and the shapes.
- * Errors: as lvspec_verify_attn.
+ * Errors: as lvspec_verify_attn; LVSPEC_EUNSUPPORTED for more than 2^21 units, a unit being 32 rows or the rest
+ * of a sequence's kv head, and for more than 2^30 units times (table_cols + 8) or rows of all kv heads.
  * ------------------------------------------------------------------------------------------- */
 typedef struct {
   lvspec_paged_cache cache;

@@ -541,6 +541,12 @@ def _dense(t, dtype, shape, *also):
     return t.data_ptr()
 
 
+def _one_device(*tensors):
+    """The kernels of a call read all of its tensors from one device."""
+    devices = {t.device for t in tensors if t is not None}
+    assert len(devices) == 1, devices
+
+
 def _call_on(device, fn, a, stream):
     """The call with the tensors' device current, which need not be the caller's."""
     if device.index == torch.cuda.current_device():
@@ -570,6 +576,7 @@ def paged_plan_args(kv_len, n_new, held, queue, state, table, *, outs, max_rows,
                     draft=False) -> PagedPlanArgs:
     i32 = torch.int32
     B, cols = table.shape
+    _one_device(kv_len, n_new, held, queue, state, table, *outs.values())
     a = PagedPlanArgs()
     a.B, a.table_cols, a.n_blocks = B, cols, queue.numel()
     a.max_rows, a.reserve, a.draft = int(max_rows), int(reserve), 1 if draft else 0
@@ -597,6 +604,7 @@ def paged_plan(kv_len, n_new, held, queue, state, table, *, max_rows, reserve=0,
 def paged_append_args(cache: PagedCache, k, v, plan) -> PagedAppendArgs:
     i32 = torch.int32
     a = PagedAppendArgs()
+    _one_device(*cache, k, v, plan["slots"], plan["row_seq"], plan["row_pos"], plan["cu_rows"])
     a.cache = _cache_struct(cache)
     n = k.shape[0]
     assert k.is_cuda and v.is_cuda and k.dtype == torch.bfloat16 and v.dtype == torch.bfloat16 and k.shape == v.shape
@@ -621,6 +629,7 @@ def verify_attn_paged_args(q, cache: PagedCache, table, kv_len, *, out, vis_begi
                            draft_mask=None, scale=0.0, lse=None, vis_mass=None) -> PagedAttnArgs:
     i32 = torch.int32
     a = PagedAttnArgs()
+    _one_device(*cache, q, table, kv_len, out, vis_begin, vis_end, lse, vis_mass)
     a.cache = _cache_struct(cache)
     B, gamma, Hq, D = q.shape
     assert q.is_cuda and out.is_cuda and q.dtype == torch.bfloat16 and out.dtype == torch.bfloat16
@@ -667,6 +676,7 @@ def paged_commit_args(cache: PagedCache, table, kv_len, accept_len, chain_len, *
     i32 = torch.int32
     layers = cache.k_pool.shape[0] if cache.k_pool.dim() == 5 else 1
     a = PagedCommitArgs()
+    _one_device(*cache, table, kv_len, accept_len, best_branch, new_len)
     a.cache = _cache_struct(cache, (layers,) if cache.k_pool.dim() == 5 else ())
     B = a.cache.B
     a.n_layers, a.n_branches, a.chain_len = layers, int(n_branches), int(chain_len)

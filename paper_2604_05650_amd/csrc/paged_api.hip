@@ -46,9 +46,10 @@ int plan_paged_attn(const lvspec_paged_attn_args* a, PagedPlan* pl) {
   pl->R = pl->G * a->gamma;
   pl->n_rc = (pl->R + 31) / 32;
   pl->rpad = ((pl->R + pl->n_rc - 1) / pl->n_rc + 3) / 4 * 4;
-  // places of all units (eight for open rows each), parts and output rows are 32-bit numbers in the kernels
+  // places of all units (eight for open rows each), parts and output rows are 32-bit numbers in the kernels, and
+  // so are the threads of a launch
   const int64_t units = (int64_t)c.B * c.Hkv * pl->n_rc;
-  if (units * ((int64_t)a->table_cols + 8) > (int64_t)1 << 30 || (int64_t)c.B * c.Hkv * pl->R > (int64_t)1 << 30)
+  if (units > 1 << 21 || units * ((int64_t)a->table_cols + 8) > (int64_t)1 << 30 || (int64_t)c.B * c.Hkv * pl->R > (int64_t)1 << 30)
     return LVSPEC_EUNSUPPORTED;
   const int cus = lvspec::num_compute_units();
   pl->limit = (int)units + cus - 1;

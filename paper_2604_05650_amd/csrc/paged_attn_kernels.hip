@@ -43,7 +43,7 @@ LVS_DEV u32x4 widen(uint32_t lo, uint32_t hi, float scale) {
 // A wave's ring: one slot of keys, one of values.  An operand read has as many tokens (or channels) as lanes and
 // would ask memory for as many rows at a time, a cache line each; copies go row by row instead, and LDS has the
 // 16-byte chunks of a row in an order in which the operand reads meet no bank twice: chunk c of token t at
-// c ^ k_place(t), chunk c of channel d at c ^ v_place(d / 4), functions of the core (Rows16, Rows32).
+// c ^ k_place(t), chunk c of channel d at c ^ v_place(d / 4), functions of the core (Rows16, WideRows).
 constexpr int kRingBytes = 2 * kPageBytes;
 
 // Eight copies of 1 KiB of a block of the pool to a slot, lane l of copy y from offset y * 1024 + o[y].  No
@@ -90,7 +90,7 @@ LVS_DEV void copy_page(const uint8_t* pool, int id, int64_t head, int n_heads, u
 // line of all units, whatever their ends: 16 x (2048 to 32768) keys 79 and 74.
 // Where lengths are so ragged that whole parts leave the longest half as long again as an even share, there
 // may be more: 32 x (500 to 60000) keys, 256 units, 298 us without this and 155 with it, 48 x (100 to 20000)
-// 125 and 89.  Everywhere, it costs: 5 x 12000, 150 rows 26.8 and 33.9, 16 x (2048 to 32768) keys 74 and 80.
+// 125 and 89.  Everywhere, it costs: 24 x 5000, 7 rows 26.8 and 33.9, 16 x (2048 to 32768) keys 74 and 80.
 constexpr int kOpenTiles = 8;
 
 LVS_DEV int wave_scan(int x) {               // inclusive sum over the lanes
@@ -301,7 +301,9 @@ struct Rows16 {
 // 17 to 32 rows, on 32x32 tiles, which leave the vector unit more room beside the matrix unit than 16x16 ones
 // (matrix instructions of one wave and FMAs of another on a SIMD: 366 us together, 238 and 307 alone; on 16x16
 // 402, 257 and 307): half a wave's lanes (h) hold a row (n32).  Key 32 kb + 16 h + r is element 16 kb + r.
-struct Rows32Core {
+// (64 rows of a wave, which would share the conversion, take 400 registers, and half of a wave's are no operands
+// of its vector instructions: 16384 keys, 150 rows 29.1 us so, in chunks of 32 23.2; 8 x 8000, 64 rows 43.8 and 40.2.)
+struct WideRows {
   static constexpr int kRows = 32, kScores = 32, kLanes = 2;
   u32x4 q[8];              // channels 16 (2 (x/2) + h) + 8 (x%2) .. +7
   f32x16 acc[4];           // O^T: channels 32 db + 8 (r/4) + 4 h + r%4
@@ -945,11 +947,11 @@ hipError_t launch_paged_attn(const PagedAttnKernelArgs& a, hipStream_t stream) {
   const bool once = a.n_rc == 1;
   const int64_t units = (int64_t)a.B * a.Hkv * a.n_rc;
   if (a.cols <= unit_columns(units, a.limit - units + 1)) {
-    if (a.rpad <= 16) return once ? launch_units<Rows16, 8, true>(a, stream) : launch_units<Rows16, 8, false>(a, stream);
-    return once ? launch_units<Rows32Core, 8, true>(a, stream) : launch_units<Rows32Core, 8, false>(a, stream);
+    if (a.rpad <= 16) return launch_units<Rows16, 8, true>(a, stream);      // (one chunk: two have 17 rows each and more)
+    return once ? launch_units<WideRows, 8, true>(a, stream) : launch_units<WideRows, 8, false>(a, stream);
   }
-  if (a.rpad <= 16) return once ? launch_parts<Rows16, 4, true>(a, stream) : launch_parts<Rows16, 4, false>(a, stream);
-  return once ? launch_parts<Rows32Core, 4, true>(a, stream) : launch_parts<Rows32Core, 4, false>(a, stream);
+  if (a.rpad <= 16) return launch_parts<Rows16, 4, true>(a, stream);
+  return once ? launch_parts<WideRows, 4, true>(a, stream) : launch_parts<WideRows, 4, false>(a, stream);
 }
 
 }  // namespace lvspec

@@ -521,3 +521,30 @@ def test_two_streams(L):
             got.append(last)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_pool_of_more_than_4_gib(L):
+    """The last blocks of a large pool hold and give what the blocks of a small one do."""
+    B, Hkv, Hq, g, prompt, chain = 2, 4, 8, 5, [200, 70], 5
+    small, far = 8, (1 << 17) + 64                      # 4 GiB and 2 MiB of keys, as much of values
+    k, v = normal(1, (sum(prompt), Hkv, D)), normal(2, (sum(prompt), Hkv, D))
+    dk, dv, q = normal(3, (B * g, Hkv, D)), normal(4, (B * g, Hkv, D)), normal(5, (B, g, Hq, D))
+    outs, ends = [], []
+    for n_blocks in (small, far):
+        st = L.alloc_paged_state(B, n_blocks, 6, DEV)
+        cache = L.alloc_paged_cache(B, Hkv, n_blocks, DEV)
+        state = i32([n_blocks - small, small])          # the last blocks are what is free
+        plan = L.paged_plan(i32([0] * B), i32(prompt), st["held"], st["queue"], state, st["table"], max_rows=sum(prompt))
+        L.paged_append(cache, k, v, plan)
+        kv_len = i32([190, 67])                         # the first's drafts complete a block
+        step = L.paged_plan(kv_len, i32([g] * B), plan["new_held"], st["queue"], plan["new_state"], st["table"],
+                            max_rows=B * g, reserve=g, draft=True)
+        L.paged_append(cache, dk, dv, step)
+        outs.append(L.verify_attn_paged(q, cache, st["table"], kv_len))
+        new_len = L.paged_commit(cache, st["table"], kv_len, i32([5, 2]), chain)
+        assert new_len.tolist() == [195, 69]
+        assert int(st["table"].max()) < n_blocks and int(st["table"][0, 0]) == n_blocks - small
+        ends.append([x[n_blocks - small:].clone().view(torch.uint8) for x in (cache.k_pool, cache.v_pool)] +
+                    [x[n_blocks - small:].clone() for x in (cache.k_scale, cache.v_scale)])
+    assert torch.equal(outs[0], outs[1])
+    assert all(torch.equal(x, y) for x, y in zip(*ends))

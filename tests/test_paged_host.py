@@ -79,7 +79,8 @@ def test_attention_refusals(L):
             (dict(o_sg=1028), -1), (dict(vis_begin=0x1000), -1), (dict(vis_mass=0x1000), -1),
             (dict(draft_mask=blind), -1), (dict(draft_mask=beyond), -1), (dict(workspace=0), L.EWORKSPACE),
             (dict(workspace=0x10010), L.EWORKSPACE), (dict(workspace_bytes=100), L.EWORKSPACE),
-            ({"cache.B": 4096, "table_cols": 1 << 20}, -2)]
+            ({"cache.B": 4096, "table_cols": 1 << 20}, -2),
+            ({"cache.B": 4096, "cache.Hkv": 1024, "Hq": 1024}, -2)]
     refused(L, "lvspec_verify_attn_paged", L.PagedAttnArgs, good, bad)
 
 
@@ -96,6 +97,13 @@ def test_attention_workspace(L):
     exact = need()
     a = fill(L.PagedAttnArgs(), {**ATTN, "workspace_bytes": exact - 1})
     assert L.raw().lvspec_verify_attn_paged(C.byref(a), None) == L.EWORKSPACE
+
+
+def test_tensors_of_a_call_are_on_one_device(L):
+    here, there = torch.empty(1), torch.empty(1, device="meta")
+    L._one_device(here, None, here)
+    with pytest.raises(AssertionError):
+        L._one_device(here, there)
 
 
 def test_commit_refusals(L):
