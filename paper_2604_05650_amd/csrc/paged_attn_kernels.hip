@@ -111,37 +111,55 @@ LVS_DEV int full_blocks(const PagedAttnKernelArgs& p, int b) { return paged_len(
 LVS_DEV int divide(int x, int d) { return (int)((uint32_t)x / (uint32_t)d); }
 LVS_DEV int about(int x, int d) { return (int)((float)x * __builtin_amdgcn_rcpf((float)d)); }
 
-// places of the units of sequences b0 .. b0+63, one per lane; 0 behind the last one
-LVS_DEV int places_of(const PagedAttnKernelArgs& p, int b) { return b < p.B ? full_blocks(p, b) + kOpenTiles : 0; }
+// Places of the units of sequences `per` lane .. `per` lane + `per` - 1; 0 behind the last one.
+constexpr int kPer = 4;
+struct Places {
+  int per, of[kPer];
+  LVS_DEV Places(const PagedAttnKernelArgs& p, int lane) : per((p.B + 63) >> 6) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int b = lane * per + i;
+      of[i] = i < per && b < p.B ? full_blocks(p, b) + kOpenTiles : 0;
+    }
+  }
+};
 
 struct Cut {
   int total;           // parts of all units
   uint32_t inv;        // about 2^32 / most places of a part
   // parts of a unit of so many places (about places / most, rounded up: any number serves that both kernels find)
   LVS_DEV int parts(int places) const { return places == 0 ? 0 : 1 + (int)__umulhi((uint32_t)(places - 1), inv); }
+  // of a unit of each of the lane's sequences
+  LVS_DEV int parts(const Places& places) const {
+    int n = parts(places.of[0]);
+#pragma unroll
+    for (int i = 1; i < kPer; ++i)
+      if (i < places.per) n += parts(places.of[i]);
+    return n;
+  }
 };
 
-// places0: those of the first 64 sequences; KS: streams of a workgroup
+// KS: streams of a workgroup
 template <int KS>
-LVS_DEV Cut cut_units(const PagedAttnKernelArgs& p, int lane, int places0) {
-  int sum = last_lane(wave_scan(places0)), most = (int)wave_max_u32((uint32_t)places0);
-  for (int b0 = 64; b0 < p.B; b0 += 64) {
-    const int x = places_of(p, b0 + lane);
-    sum += last_lane(wave_scan(x));
-    most = max(most, (int)wave_max_u32((uint32_t)x));
+LVS_DEV Cut cut_units(const PagedAttnKernelArgs& p, const Places& places) {
+  int sum = places.of[0], most = places.of[0];
+#pragma unroll
+  for (int i = 1; i < kPer; ++i) {
+    sum += places.of[i];
+    most = max(most, places.of[i]);
   }
+  sum = last_lane(wave_scan(sum));
+  most = (int)wave_max_u32((uint32_t)most);
   const int HR = p.Hkv * p.n_rc;
   Cut c;
-  int limit = p.limit - p.spare, part = 0;
+  int limit = p.limit - p.spare;
   while (true) {
     const int even = about(sum * HR, limit);
     // whole rounds of the streams: a part of 4 k + 1 tiles takes as long as one of 4 (k + 1)
-    part = max((even + KS - 1) / KS * KS, kOpenTiles);
+    int part = max((even + KS - 1) / KS * KS, kOpenTiles);
     while (true) {
       c.inv = (uint32_t)(4294967040.f * __builtin_amdgcn_rcpf((float)part));
-      int n = last_lane(wave_scan(c.parts(places0)));
-      for (int b0 = 64; b0 < p.B; b0 += 64) n += last_lane(wave_scan(c.parts(places_of(p, b0 + lane))));
-      c.total = n * HR;
+      c.total = last_lane(wave_scan(c.parts(places))) * HR;
       if (c.total <= limit) break;            // (one part each serves, so it ends)
       part += max(part >> 3, KS) / KS * KS;
     }
@@ -759,24 +777,27 @@ __global__ __launch_bounds__(64 * KS, 2) void paged_attn_kernel(PagedAttnKernelA
   extern __shared__ __align__(256) uint8_t smem[];
   Segment<Rows, KS, ONCE> sg(p, smem);
   const int HR = p.Hkv * p.n_rc, lane = threadIdx.x & 63;
-  int places = places_of(p, lane);
-  const Cut cut = cut_units<KS>(p, lane, places);
+  const Places places(p, lane);
+  const Cut cut = cut_units<KS>(p, places);
   // parts that follow each other go to one XCD, which has the records of a unit in its L2
   const int each = (cut.total + 7) >> 3;
   const int w = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
   if ((int)(blockIdx.x >> 3) >= each || w >= cut.total) return;
-  int b0 = 0, upto = wave_scan(cut.parts(places));       // sequences b0 .. b0+63 at hand
-  while (w >= last_lane(upto) * HR) {                     // (ends: w < total)
-    const int before = last_lane(upto);
-    b0 += 64;
-    places = places_of(p, b0 + lane);
-    upto = before + wave_scan(cut.parts(places));
-  }
-  const int in = __popcll(__ballot(w >= upto * HR));
-  const int unit_places = __builtin_amdgcn_readlane(places, in), n = cut.parts(unit_places);
-  const int y = w - (__builtin_amdgcn_readlane(upto, in) - n) * HR;
+  const int f = cut.parts(places), upto = wave_scan(f);
+  const int holder = __popcll(__ballot(w >= upto * HR));      // the lane that has the sequence
+  int b = holder * places.per, before = __builtin_amdgcn_readlane(upto - f, holder);
+  int unit_places = __builtin_amdgcn_readlane(places.of[0], holder), n = cut.parts(unit_places);
+#pragma unroll
+  for (int i = 1; i < kPer; ++i)
+    if (i < places.per && w >= (before + n) * HR) {
+      before += n;
+      ++b;
+      unit_places = __builtin_amdgcn_readlane(places.of[i], holder);
+      n = cut.parts(unit_places);
+    }
+  const int y = w - before * HR;
   const int hr = divide(y, n), part = y - hr * n;
-  const int b = b0 + in, h = ONCE ? hr : divide(hr, p.n_rc), rc = hr - h * p.n_rc;
+  const int h = ONCE ? hr : divide(hr, p.n_rc), rc = hr - h * p.n_rc;
   const int q = divide(unit_places, n), r = unit_places - q * n;      // the first r parts have one more
   const int p0 = part * q + min(part, r), p1 = p0 + q + (part < r ? 1 : 0);
   const int t0 = max(p0 - kOpenTiles, 0), t1 = p1 - kOpenTiles;
@@ -825,20 +846,17 @@ __global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(PagedAtt
   const int in = (blockIdx.x - unit * per_unit) * kRows + g / SPLIT, r = rc * p.rpad + in;
   const bool row = in < p.rpad && r < p.R;
   // the unit's records
-  int places = places_of(p, lane);
-  const Cut cut = cut_units<KS>(p, lane, places);
-  int before = 0, n = 0;
-  for (int b0 = 0; b0 <= b; b0 += 64) {
-    if (b0 > 0) places = places_of(p, b0 + lane);
-    const int f = cut.parts(places);
-    const int upto = wave_scan(f);
-    if (b < b0 + 64) {
-      n = __builtin_amdgcn_readlane(f, b - b0);
-      before += __builtin_amdgcn_readlane(upto, b - b0) - n;
-    } else {
-      before += last_lane(upto);
+  const Places places(p, lane);
+  const Cut cut = cut_units<KS>(p, places);
+  const int f = cut.parts(places), holder = (int)((uint32_t)b / (uint32_t)places.per);      // (a lane)
+  int before = __builtin_amdgcn_readlane(wave_scan(f) - f, holder);
+  int n = cut.parts(__builtin_amdgcn_readlane(places.of[0], holder));
+#pragma unroll
+  for (int i = 1; i < kPer; ++i)
+    if (i <= b - holder * places.per) {
+      before += n;
+      n = cut.parts(__builtin_amdgcn_readlane(places.of[i], holder));
     }
-  }
   if (n == 1) return;                            // (one part: it has written the output)
   const int64_t step = (int64_t)p.rpad * 131;
   const float* rec = record_at(p, before * HR + hr * n) + (row ? in : 0);
@@ -908,8 +926,11 @@ __global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(PagedAtt
 // have as many blocks, so the more units there are, the more of them pay: they fill the chip anyway.  One
 // workgroup per unit and parts, us: 8 units 800 keys 11.1 and 12.4, 1100 12.2 and 12.7, 1400 13.9 and 12.7;
 // 64 units 1000 keys 13.3 and 13.8, 1500 15.9 and 14.4; 128 units 2000 keys 18.6 and 20.7, 3000 24.6 and 26.1;
-// 256 units 4000 keys 45.9 and 49.8, 512 units 91.6 and 89.6.
-int unit_columns(int64_t units, int64_t cus) { return units >= cus / 2 ? 64 : 18; }
+// 256 units 4000 keys 45.9 and 49.8, 512 units 91.6 and 89.6.  More than 64 kPer sequences are not cut, whose places
+// a wave cannot hold: 250 x (400 to 12000) keys, 2 heads 96 and 92.
+int unit_columns(int64_t B, int64_t units, int64_t cus) {
+  return B > 64 * kPer ? 1 << 30 : units >= cus / 2 ? 64 : 18;
+}
 
 template <class Rows, int KS, bool ONCE>
 hipError_t launch_parts(const PagedAttnKernelArgs& a, hipStream_t stream) {
@@ -946,7 +967,7 @@ hipError_t launch_units(const PagedAttnKernelArgs& a, hipStream_t stream) {
 hipError_t launch_paged_attn(const PagedAttnKernelArgs& a, hipStream_t stream) {
   const bool once = a.n_rc == 1;
   const int64_t units = (int64_t)a.B * a.Hkv * a.n_rc;
-  if (a.cols <= unit_columns(units, a.limit - units + 1)) {
+  if (a.cols <= unit_columns(a.B, units, a.limit - units + 1)) {
     if (a.rpad <= 16) return launch_units<Rows16, 8, true>(a, stream);      // (one chunk: two have 17 rows each and more)
     return once ? launch_units<WideRows, 8, true>(a, stream) : launch_units<WideRows, 8, false>(a, stream);
   }

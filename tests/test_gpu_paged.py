@@ -252,6 +252,8 @@ ATTNS = [
     dict(kv=[1200, 300] + [17] * 60, g=1, Hq=8, Hkv=8), dict(kv=[9600] * 10 + [20] * 50, g=1, Hq=8, Hkv=8),
     dict(kv=[25000, 24000, 26000], g=1, Hq=16, Hkv=16), dict(kv=[(53 * i) % 300 for i in range(70)], g=2, Hq=8, Hkv=8),
     dict(kv=[(53 * i) % 300 for i in range(131)] + [5000, 0, 64, 9000], g=3, Hq=2, Hkv=1),
+    dict(kv=[7000, 0] + [(71 * i) % 200 for i in range(252)] + [64, 6000], g=1, Hq=2, Hkv=1),       # as many as are cut
+    dict(kv=[(71 * i) % 200 for i in range(256)] + [6500], g=1, Hq=2, Hkv=1),                       # and one more
 ]
 
 
