@@ -298,7 +298,7 @@ struct PagedAttnKernelArgs {
   int64_t o_sb, o_sg, o_sh;
   float* lse;
   float* vis_mass;
-  float* ws;                    // limit records of rpad * 131 floats
+  float* ws;                    // limit records of rpad * 131 floats, and two numbers per unit
   uint32_t draft_mask[32];
 };
 hipError_t launch_paged_attn(const PagedAttnKernelArgs& a, hipStream_t stream);

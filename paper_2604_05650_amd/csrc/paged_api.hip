@@ -54,7 +54,7 @@ int plan_paged_attn(const lvspec_paged_attn_args* a, PagedPlan* pl) {
   const int cus = lvspec::num_compute_units();
   pl->limit = (int)units + cus - 1;
   pl->spare = pl->limit - std::max((int)units, cus);
-  pl->ws_bytes = (size_t)pl->limit * pl->rpad * 131 * sizeof(float);
+  pl->ws_bytes = (size_t)pl->limit * pl->rpad * 131 * sizeof(float) + (size_t)units * 8;
   return LVSPEC_OK;
 }
 

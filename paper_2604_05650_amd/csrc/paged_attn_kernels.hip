@@ -82,7 +82,8 @@ LVS_DEV void copy_page(const uint8_t* pool, int id, int64_t head, int n_heads, u
 // A unit has kOpenTiles places for its open rows, which take about as long as so many tiles, and a place per
 // tile of 64 keys.  Every unit is cut into equal parts of at most so many places that there are no more parts
 // than compute units (or units, if they are more); who has the first of a unit's places does its open rows.
-// The lengths are on the device, so every wave finds the cut and its place by itself.
+// The lengths are on the device, so every wave finds the cut and its place by itself; a unit's first part
+// leaves a note of its records for the merge.
 // One workgroup of four waves per CU draws the 27 GB/s that are the CU's share of the memory's rate, and each
 // part has 5 us of its own (first loads, merge, record).  For two per CU: 8 x 8000 keys, 40/8 heads, 8 rows
 // 46.2 us against 38.5 here, 2 x 16000, 30 rows 50.4 and 44.8, 32 x 6000, 5 rows 84 and 69; eight waves in one
@@ -116,10 +117,16 @@ constexpr int kPer = 4;
 struct Places {
   int per, of[kPer];
   LVS_DEV Places(const PagedAttnKernelArgs& p, int lane) : per((p.B + 63) >> 6) {
+    of[0] = lane * per < p.B ? full_blocks(p, lane * per) + kOpenTiles : 0;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int b = lane * per + i;
-      of[i] = i < per && b < p.B ? full_blocks(p, b) + kOpenTiles : 0;
+    for (int i = 1; i < kPer; ++i) of[i] = 0;
+    if (per > 1) {
+      asm volatile("");
+#pragma unroll
+      for (int i = 1; i < kPer; ++i) {
+        const int b = lane * per + i;
+        of[i] = i < per && b < p.B ? full_blocks(p, b) + kOpenTiles : 0;
+      }
     }
   }
 };
@@ -127,14 +134,16 @@ struct Places {
 struct Cut {
   int total;           // parts of all units
   uint32_t inv;        // about 2^32 / most places of a part
-  // parts of a unit of so many places (about places / most, rounded up: any number serves that both kernels find)
+  // parts of a unit of so many places: about places / most, rounded up
   LVS_DEV int parts(int places) const { return places == 0 ? 0 : 1 + (int)__umulhi((uint32_t)(places - 1), inv); }
   // of a unit of each of the lane's sequences
   LVS_DEV int parts(const Places& places) const {
     int n = parts(places.of[0]);
+    if (places.per > 1) {
+      asm volatile("");                  // (a jump, not four times the instructions)
 #pragma unroll
-    for (int i = 1; i < kPer; ++i)
-      if (i < places.per) n += parts(places.of[i]);
+      for (int i = 1; i < kPer; ++i) n += parts(places.of[i]);
+    }
     return n;
   }
 };
@@ -143,10 +152,13 @@ struct Cut {
 template <int KS>
 LVS_DEV Cut cut_units(const PagedAttnKernelArgs& p, const Places& places) {
   int sum = places.of[0], most = places.of[0];
+  if (places.per > 1) {
+    asm volatile("");
 #pragma unroll
-  for (int i = 1; i < kPer; ++i) {
-    sum += places.of[i];
-    most = max(most, places.of[i]);
+    for (int i = 1; i < kPer; ++i) {
+      sum += places.of[i];
+      most = max(most, places.of[i]);
+    }
   }
   sum = last_lane(wave_scan(sum));
   most = (int)wave_max_u32((uint32_t)most);
@@ -770,7 +782,9 @@ struct Segment {
   }
 };
 
+// Workspace: a record per part, and a unit's first record and their number.
 LVS_DEV float* record_at(const PagedAttnKernelArgs& p, int64_t i) { return p.ws + i * ((int64_t)p.rpad * 131); }
+LVS_DEV int2* records_of(const PagedAttnKernelArgs& p) { return reinterpret_cast<int2*>(record_at(p, p.limit)); }
 
 template <class Rows, int KS, bool ONCE>
 __global__ __launch_bounds__(64 * KS, 2) void paged_attn_kernel(PagedAttnKernelArgs p) {
@@ -801,6 +815,7 @@ __global__ __launch_bounds__(64 * KS, 2) void paged_attn_kernel(PagedAttnKernelA
   const int q = divide(unit_places, n), r = unit_places - q * n;      // the first r parts have one more
   const int p0 = part * q + min(part, r), p1 = p0 + q + (part < r ? 1 : 0);
   const int t0 = max(p0 - kOpenTiles, 0), t1 = p1 - kOpenTiles;
+  if (part == 0 && threadIdx.x == 0) records_of(p)[b * HR + hr] = int2{w, n};
   const int L = p0 == 0 ? paged_len(p.kv_len[b], p.cols) : 0;      // (for the open rows)
   sg.begin(b, h, rc);
   if (p0 == 0) sg.open_rows(b, h, rc, L);
@@ -831,13 +846,13 @@ __global__ __launch_bounds__(64 * KS, 2) void paged_attn_unit_kernel(PagedAttnKe
 // all eight of a workgroup where a unit has many records, or one group per row.
 constexpr int kCombineThreads = 256;
 
-template <int SPLIT, int KS>
+template <int SPLIT>
 __global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(PagedAttnKernelArgs p) {
   constexpr int kRows = 8 / SPLIT;               // output rows of a workgroup, all of one unit
   constexpr int kAhead = 8;
   __shared__ float s_m[8], s_l[8], s_v[8];
   __shared__ f32x4 s_o[SPLIT > 1 ? 8 : 1][32];
-  const int tid = threadIdx.x, lane = tid & 63, g = tid >> 5, l32 = tid & 31;
+  const int tid = threadIdx.x, g = tid >> 5, l32 = tid & 31;
   const int HR = p.Hkv * p.n_rc;
   const int per_unit = (p.rpad + kRows - 1) / kRows;
   const int unit = (int)((uint32_t)blockIdx.x / (uint32_t)per_unit);
@@ -845,21 +860,11 @@ __global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(PagedAtt
   const int h = (int)((uint32_t)hr / (uint32_t)p.n_rc), rc = hr - h * p.n_rc;
   const int in = (blockIdx.x - unit * per_unit) * kRows + g / SPLIT, r = rc * p.rpad + in;
   const bool row = in < p.rpad && r < p.R;
-  // the unit's records
-  const Places places(p, lane);
-  const Cut cut = cut_units<KS>(p, places);
-  const int f = cut.parts(places), holder = (int)((uint32_t)b / (uint32_t)places.per);      // (a lane)
-  int before = __builtin_amdgcn_readlane(wave_scan(f) - f, holder);
-  int n = cut.parts(__builtin_amdgcn_readlane(places.of[0], holder));
-#pragma unroll
-  for (int i = 1; i < kPer; ++i)
-    if (i <= b - holder * places.per) {
-      before += n;
-      n = cut.parts(__builtin_amdgcn_readlane(places.of[i], holder));
-    }
-  if (n == 1) return;                            // (one part: it has written the output)
+  const int2 own = records_of(p)[unit];
+  if (own.y == 1) return;                        // (one part: it has written the output)
+  const int n = own.y;
   const int64_t step = (int64_t)p.rpad * 131;
-  const float* rec = record_at(p, before * HR + hr * n) + (row ? in : 0);
+  const float* rec = record_at(p, own.x) + (row ? in : 0);
   // every group for itself: maximum, sums and output of its records, eight at a time
   float mm = kNegBig, l = 0.f, lv = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -945,9 +950,9 @@ hipError_t launch_parts(const PagedAttnKernelArgs& a, hipStream_t stream) {
   // few units have many records each: all groups of a workgroup to one row.  8 units, 32 records each: 16.4 us
   // so and 17.7 with a group per row; 64 units, 4 each: 23.9 and 20.9.
   if ((int64_t)units * 16 > a.limit - a.spare)
-    paged_combine_kernel<1, KS><<<dim3(units * (unsigned)((a.rpad + 7) / 8)), dim3(kCombineThreads), 0, stream>>>(a);
+    paged_combine_kernel<1><<<dim3(units * (unsigned)((a.rpad + 7) / 8)), dim3(kCombineThreads), 0, stream>>>(a);
   else
-    paged_combine_kernel<8, KS><<<dim3(units * (unsigned)a.rpad), dim3(kCombineThreads), 0, stream>>>(a);
+    paged_combine_kernel<8><<<dim3(units * (unsigned)a.rpad), dim3(kCombineThreads), 0, stream>>>(a);
   return hipGetLastError();
 }
 
