@@ -11,6 +11,9 @@ namespace {
 // workgroup takes them by itself, 16 requests per thread at most, and then fills its share of the rows and
 // of the table: one launch, no state changed in place, so that a second call on the same input gives the
 // same answer.  Sums saturate just above what is compared with.
+// Bound by latency: lengths, three sums one behind the other, a search for the row's request, the queue.  16
+// requests with 5 drafts each 4.8 us, 64 prompts of 1000 to 16384 rows 9.0 us, of which the 4.2 MB written
+// are 1.
 constexpr int kPlanThreads = 256;
 constexpr int kPlanMaxB = 4096;
 constexpr int kPlanRows = 4;       // rows per thread and turn
@@ -254,7 +257,9 @@ LVS_DEV void store_block(const u32x4 (&x)[4], bool turned, uint8_t* dst, float* 
 // ------------------------------------------------------------------------------ append
 // One workgroup per 64 packed rows, kv head and tensor.  A block belongs to the workgroup that finds its
 // last row; its first rows may be the packed rows of the tiles before or, where they came in an earlier
-// call, rows of the ring.
+// call, rows of the ring.  Every row is read once and every block written once: bound by memory, 4.6 to 5.3 TB/s
+// of reads and writes (16384 rows, 8 heads 19 to 22 us, 12 x (300 to 9000) rows 41), where a torch copy reaches
+// 4.9; the turn of the values through LDS, a third of whose cycles are bank conflicts, hides behind that.
 __global__ __launch_bounds__(kCacheThreads) void paged_append_kernel(AppendKernelArgs a) {
   __shared__ __align__(16) uint32_t s_turn[kTurnDwords];
   __shared__ uint32_t s_max[4];
@@ -338,6 +343,9 @@ __global__ __launch_bounds__(kCacheThreads) void paged_append_kernel(AppendKerne
 // One workgroup per (sequence, kv head), tensor and layer: the kept chain's accepted rows move to the front
 // of the draft area, and the block that they complete goes into the pool.  Both read the rows where the step
 // left them; what is written (rows L .. L+tau-1, and the pool) is read by neither.
+// All layers in one launch: a layer alone would be mostly launch.  Bound by memory where blocks become complete:
+// 64 layers, 8 heads, 1 sequence 7.5 us for 25 MB, of which 3 are launch and lengths; 16 sequences with two
+// chains of 10, a quarter of them with a block, 27 us for 126 MB, 4.6 TB/s.
 __global__ __launch_bounds__(kCacheThreads) void paged_commit_kernel(PagedCommitKernelArgs a) {
   __shared__ __align__(16) uint32_t s_turn[kTurnDwords];
   __shared__ uint32_t s_max[4];
