@@ -126,6 +126,10 @@ GROUPS = {   # kernels launched by one call of each entry point
                        "accept_finalize_kernel", "accept_merge_kernel", "accept_rule_kernel"),
     "kv_commit": ("kv_commit_kernel",),
     "hv_prepare": ("hv_prepare_kernel",),
+    "paged_plan": ("paged_plan_kernel",),
+    "paged_append": ("paged_append_kernel",),
+    "verify_attn_paged": ("paged_attn_kernel", "paged_attn_unit_kernel", "paged_combine_kernel"),
+    "paged_commit": ("paged_commit_kernel",),
 }
 # of these, the kernels that stream, by the start of their names
 STREAMS = {
