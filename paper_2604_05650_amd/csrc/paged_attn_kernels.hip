@@ -574,6 +574,7 @@ struct Segment {
     auto copy_v = [&](int id) { copy_page<ONCE>(p.v8, id, h, p.Hkv, v_slot, v_off); };
     fetch(0);
     int id = __builtin_amdgcn_readlane(ids, 0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (the open rows' reads of the ring)
     copy_k(id);
     copy_v(id);
     float k_scale = scale_of(p.k_scale, id), v_scale = scale_of(p.v_scale, id);
