@@ -18,7 +18,7 @@
 // Bound: the streaming read of K and V from memory, 16 x (2048 to 32768) keys, 8 heads, 5 rows of 5 heads 70 us for
 // 367 MB, 5.2 TB/s; of short ones the start, the merge and the second launch, 16384 keys 13.2 + 4.0 us for
 // 34 MB; of 33 and more rows the vector instructions, which every chunk of 32 has for itself (16384 keys, 100
-// rows: 20.8 us, vector unit 35 % busy, matrix unit 17 to 19 %, a wave alone on its SIMD; 4 x 65536 keys,
+// rows: 19 to 20 us, vector unit 37 % busy, matrix unit 18 %, start and merge among them; 4 x 65536 keys,
 // 64 rows 110 us for 540 MB, 4.9 TB/s, matrix unit 25 %).
 #include "attn_rows32.h"
 #include "paged_dev.h"
@@ -89,13 +89,13 @@ LVS_DEV void copy_page(const uint8_t* pool, int id, int64_t head, int n_heads, u
 // leaves a note of its records for the merge.
 // One workgroup of four waves per CU draws the 27 GB/s that are the CU's share of the memory's rate, and each
 // part has 5 us of its own (first loads, merge, record).  For two per CU: 8 x 8000 keys, 40/8 heads, 8 rows
-// 46.2 us against 38.5 here, 2 x 16000, 30 rows 50.4 and 44.8, 32 x 6000, 5 rows 84 and 69; eight waves in one
-// workgroup: 16384 keys 19.7 and 17.2, 4 x 65536, 64/8 heads, 8 rows 123 and 128.  Equal stretches of one
-// line of all units, whatever their ends: 16 x (2048 to 32768) keys 79 and 74.
+// 46.2 us against 38.5 here, 2 x 16000, 30 rows 50.4 and 44.8, 32 x 6000, 5 rows 84 and 69; equal
+// stretches of one line of all units, whatever their ends: 16 x (2048 to 32768) keys 79 and 74.
 // Where lengths are so ragged that whole parts leave the longest half as long again as an even share, there
 // may be more: 32 x (500 to 60000) keys, 256 units, 298 us without this and 155 with it, 48 x (100 to 20000)
 // 125 and 89.  Everywhere, it costs: 24 x 5000, 7 rows 26.8 and 33.9, 16 x (2048 to 32768) keys 74 and 80.
 constexpr int kOpenTiles = 8;
+constexpr int kRound = 4;          // tiles that four streams take at a time; any number: 16384 keys 16.7, so 16.0
 
 LVS_DEV int wave_scan(int x) {               // inclusive sum over the lanes
   auto add = [&](uint32_t y) { x += (int)y; };
@@ -151,8 +151,6 @@ struct Cut {
   }
 };
 
-// KS: streams of a workgroup
-template <int KS>
 LVS_DEV Cut cut_units(const PagedAttnKernelArgs& p, const Places& places) {
   int sum = places.of[0], most = places.of[0];
   if (places.per > 1) {
@@ -170,13 +168,12 @@ LVS_DEV Cut cut_units(const PagedAttnKernelArgs& p, const Places& places) {
   int limit = p.limit - p.spare;
   while (true) {
     const int even = about(sum * HR, limit);
-    // whole rounds of the streams: a part of 4 k + 1 tiles takes as long as one of 4 (k + 1)
-    int part = max((even + KS - 1) / KS * KS, kOpenTiles);
+    int part = max((even + kRound - 1) / kRound * kRound, kOpenTiles);
     while (true) {
       c.inv = (uint32_t)(4294967040.f * __builtin_amdgcn_rcpf((float)part));
       c.total = last_lane(wave_scan(c.parts(places))) * HR;
       if (c.total <= limit) break;            // (one part each serves, so it ends)
-      part += max(part >> 3, KS) / KS * KS;
+      part += max(part >> 3, kRound) / kRound * kRound;
     }
     if (limit == p.limit || min(part, most) <= even + (even >> 1) + kOpenTiles) return c;
     limit = p.limit;
@@ -796,7 +793,7 @@ __global__ __launch_bounds__(64 * KS, 2) void paged_attn_kernel(PagedAttnKernelA
   Segment<Rows, KS, ONCE> sg(p, smem);
   const int HR = p.Hkv * p.n_rc, lane = threadIdx.x & 63;
   const Places places(p, lane);
-  const Cut cut = cut_units<KS>(p, places);
+  const Cut cut = cut_units(p, places);
   // parts that follow each other go to one XCD, which has the records of a unit in its L2
   const int each = (cut.total + 7) >> 3;
   const int w = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
@@ -978,10 +975,17 @@ hipError_t launch_units(const PagedAttnKernelArgs& a, hipStream_t stream) {
 hipError_t launch_paged_attn(const PagedAttnKernelArgs& a, hipStream_t stream) {
   const bool once = a.n_rc == 1;
   const int64_t units = (int64_t)a.B * a.Hkv * a.n_rc;
-  if (a.cols <= unit_columns(a.B, units, a.limit - units + 1)) {
+  const int64_t cus = a.limit - units + 1;
+  if (a.cols <= unit_columns(a.B, units, cus)) {
     if (a.rpad <= 16) return launch_units<Rows16, 8, true>(a, stream);      // (one chunk: two have 17 rows each and more)
     return once ? launch_units<WideRows, 8, true>(a, stream) : launch_units<WideRows, 8, false>(a, stream);
   }
+  // More than 64 rows are bound by vector instructions, beside which the matrix unit has more to do with two waves on a
+  // SIMD.  But then one workgroup fills a CU, and parts beyond the compute units wait for a second turn: that
+  // is for few units only.  Four and eight streams, us: 16384 keys, 100 rows 22.8 and 21.4; 2 x 16000, 150 rows 40.6 and
+  // 36.8; 5 x (1000 to 20000), 100 rows, 160 units 38.0 and 36.1; 6 of them, 192 units 47.7 and 54.3; 64 rows 12 x
+  // (1000 to 20000) 54.4 and 59.7; 25 rows, 16384 keys 16.0 and 16.9.
+  if (a.n_rc >= 3 && units * 8 <= cus * 5) return launch_parts<WideRows, 8, false>(a, stream);
   if (a.rpad <= 16) return launch_parts<Rows16, 4, true>(a, stream);
   return once ? launch_parts<WideRows, 4, true>(a, stream) : launch_parts<WideRows, 4, false>(a, stream);
 }

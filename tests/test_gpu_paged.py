@@ -254,6 +254,7 @@ ATTNS = [
     dict(kv=[(53 * i) % 300 for i in range(131)] + [5000, 0, 64, 9000], g=3, Hq=2, Hkv=1),
     dict(kv=[7000, 0] + [(71 * i) % 200 for i in range(252)] + [64, 6000], g=1, Hq=2, Hkv=1),       # as many as are cut
     dict(kv=[(71 * i) % 200 for i in range(256)] + [6500], g=1, Hq=2, Hkv=1),                       # and one more
+    dict(kv=[6000, 300], g=24, Hq=20, Hkv=4), dict(kv=[3000, 9000, 64, 0, 5], g=15, Hq=14, Hkv=2),  # 120 and 105 rows
 ]
 
 
