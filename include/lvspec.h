@@ -331,7 +331,10 @@ int lvspec_kv_commit(const lvspec_commit_args* args, void* stream);
  *
  * A decode loop:  plan(n_new = prompt rows) and append per layer; then per step plan(draft = 1, n_new =
  * reserve = draft rows), append or a plain copy of the draft rows into the ring, attention, acceptance,
- * commit of all layers.  Only device memory is read, so steps can be captured into a graph.
+ * commit of all layers with what the plan granted.  Only device memory is read, so steps can be captured
+ * into a graph.  A request that is not granted has its rows stored nowhere: kv_len grows by a prompt's rows
+ * only where they were granted, what attention and acceptance give for a refused draft means nothing, and
+ * commit, given the plan's outputs, leaves that sequence as it is until a later step is granted.
  * ------------------------------------------------------------------------------------------- */
 #define LVSPEC_PAGE_TOKENS 64
 #define LVSPEC_TAIL_ROWS 128
@@ -457,9 +460,16 @@ int lvspec_verify_attn_paged(const lvspec_paged_attn_args* args, void* stream);
  * kv_len[b] + tau; when kept > 0 the ring rows of positions kv_len[b] + kept*chain_len + i become those
  * of kv_len[b] + i, i < tau; and a block that becomes complete is rounded to 8 bits into block
  * table[b, kv_len[b] / 64], in every layer.  A sequence whose block has no place there (column behind the
- * table, or an entry outside the pool: it was not granted) or whose kv_len is out of range is left as it
- * is, new_len[b] = kv_len[b].
- * Errors: LVSPEC_EINVAL for NULL / out-of-range arguments or new_len aliasing kv_len.
+ * table, or an entry outside the pool) or whose kv_len is out of range is left as it is, new_len[b] =
+ * kv_len[b].
+ * granted, held and cu_rows are the granted, new_held and cu_rows of the step's lvspec_paged_plan.  With
+ * them a sequence that was not granted, or whose block is none of the held[b] that it owns, is left as it
+ * is too, and tau is no more than the rows that it brought: cu_rows[b+1] - cu_rows[b] - kept*chain_len.
+ * The table alone does not tell: a row of it keeps the entries of blocks that went back to the queue, and
+ * may have gone to others since.  Without them (all three NULL) the caller answers for every sequence with
+ * accept_len > 0 having been granted its rows.
+ * Errors: LVSPEC_EINVAL for NULL / out-of-range arguments, some but not all of granted, held and cu_rows,
+ * or new_len aliasing kv_len.
  * ------------------------------------------------------------------------------------------- */
 typedef struct {
   lvspec_paged_cache cache;         /* of the first layer */
@@ -471,6 +481,9 @@ typedef struct {
   const int32_t* accept_len;        /* DEVICE [B * n_branches] */
   const int32_t* best_branch;       /* DEVICE [B] or NULL */
   int32_t* new_len;                 /* DEVICE out [B]; must not alias kv_len */
+  const int32_t* granted;           /* DEVICE [B] of the step's plan, or NULL */
+  const int32_t* held;              /* DEVICE [B], its new_held; NULL when granted is */
+  const int32_t* cu_rows;           /* DEVICE [B + 1]; NULL when granted is */
 } lvspec_paged_commit_args;
 
 int lvspec_paged_commit(const lvspec_paged_commit_args* args, void* stream);

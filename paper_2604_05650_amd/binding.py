@@ -147,6 +147,7 @@ class PagedCommitArgs(C.Structure):
         ("table", C.c_void_p), ("table_cols", C.c_int32),
         ("kv_len", C.c_void_p), ("accept_len", C.c_void_p), ("best_branch", C.c_void_p),
         ("new_len", C.c_void_p),
+        ("granted", C.c_void_p), ("held", C.c_void_p), ("cu_rows", C.c_void_p),
     ]
 
 
@@ -672,11 +673,12 @@ def verify_attn_paged(q, cache: PagedCache, table, kv_len, *, vis_begin=None, vi
 
 
 def paged_commit_args(cache: PagedCache, table, kv_len, accept_len, chain_len, *, best_branch=None, n_branches=1,
-                      new_len) -> PagedCommitArgs:
+                      new_len, plan=None) -> PagedCommitArgs:
     i32 = torch.int32
     layers = cache.k_pool.shape[0] if cache.k_pool.dim() == 5 else 1
     a = PagedCommitArgs()
-    _one_device(*cache, table, kv_len, accept_len, best_branch, new_len)
+    given = () if plan is None else (plan["granted"], plan["new_held"], plan["cu_rows"])
+    _one_device(*cache, table, kv_len, accept_len, best_branch, new_len, *given)
     a.cache = _cache_struct(cache, (layers,) if cache.k_pool.dim() == 5 else ())
     B = a.cache.B
     a.n_layers, a.n_branches, a.chain_len = layers, int(n_branches), int(chain_len)
@@ -684,16 +686,20 @@ def paged_commit_args(cache: PagedCache, table, kv_len, accept_len, chain_len, *
     a.kv_len, a.new_len = _dense(kv_len, i32, (B,)), _dense(new_len, i32, (B,))
     a.accept_len = _dense(accept_len, i32, (B * max(1, int(n_branches)),))
     a.best_branch = None if best_branch is None else _dense(best_branch, i32, (B,))
+    if plan is not None:
+        a.granted, a.held, a.cu_rows = (_dense(x, i32, (n,)) for x, n in zip(given, (B, B, B + 1)))
     return a
 
 
 def paged_commit(cache: PagedCache, table, kv_len, accept_len, chain_len, *, best_branch=None, n_branches=1,
-                 new_len=None, stream=None):
+                 new_len=None, plan=None, stream=None):
     """lvspec_paged_commit.  cache of one layer, or of all with a leading dimension; accept_len int32
-    [B*n_branches], best_branch int32 [B] (trees).  Returns new_len int32 [B]."""
+    [B*n_branches], best_branch int32 [B] (trees); plan: what the step's paged_plan returned, by which
+    refused sequences are left as they are (None: the caller answers for all having been granted).
+    Returns new_len int32 [B]."""
     if new_len is None:
         new_len = torch.empty_like(kv_len)
     a = paged_commit_args(cache, table, kv_len, accept_len, chain_len, best_branch=best_branch,
-                          n_branches=n_branches, new_len=new_len)
+                          n_branches=n_branches, new_len=new_len, plan=plan)
     _call_on(table.device, _lib.lvspec_paged_commit, a, stream)
     return new_len

@@ -269,6 +269,9 @@ struct PagedCommitKernelArgs {
   const int32_t* kv_len;
   const int32_t* accept_len;
   const int32_t* best_branch;   // optional
+  const int32_t* granted;       // optional, and with it held and cu_rows
+  const int32_t* held;
+  const int32_t* cu_rows;
   int32_t* new_len;
   int B, Hkv, n_layers, n_branches, chain_len, n_blocks, cols;
 };

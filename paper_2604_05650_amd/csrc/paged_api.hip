@@ -176,12 +176,15 @@ int lvspec_paged_commit(const lvspec_paged_commit_args* a, void* stream) {
   rc = check_cache_pointers(&c);
   if (rc != LVSPEC_OK) return rc;
   if (!a->table || !a->kv_len || !a->accept_len || !a->new_len || a->new_len == a->kv_len) return LVSPEC_EINVAL;
+  if ((a->granted == nullptr) != (a->held == nullptr) || (a->granted == nullptr) != (a->cu_rows == nullptr))
+    return LVSPEC_EINVAL;
   lvspec::PagedCommitKernelArgs k{};
   k.k8 = static_cast<uint8_t*>(c.k_pool); k.v8 = static_cast<uint8_t*>(c.v_pool);
   k.k_scale = c.k_scale; k.v_scale = c.v_scale;
   k.k_tail = static_cast<uint8_t*>(c.k_tail); k.v_tail = static_cast<uint8_t*>(c.v_tail);
   k.table = a->table; k.kv_len = a->kv_len; k.accept_len = a->accept_len;
   k.best_branch = nbr > 1 ? a->best_branch : nullptr;
+  k.granted = a->granted; k.held = a->held; k.cu_rows = a->cu_rows;
   k.new_len = a->new_len;
   k.B = c.B; k.Hkv = c.Hkv; k.n_layers = a->n_layers; k.n_branches = nbr; k.chain_len = a->chain_len;
   k.n_blocks = c.n_blocks; k.cols = a->table_cols;

@@ -359,12 +359,22 @@ __global__ __launch_bounds__(kCacheThreads) void paged_commit_kernel(PagedCommit
   int tau = a.accept_len[b * a.n_branches + kept];
   tau = tau < 0 ? 0 : tau > a.chain_len ? a.chain_len : tau;
   const int col = L >> kPageShift;
+  // The table keeps entries of blocks that were given back, so what a sequence has is told by the plan: rows that
+  // were not granted are not in the ring, and a block behind the held ones is another sequence's.
+  bool granted = true;
+  int held = a.cols;
+  if (a.granted != nullptr) {
+    granted = a.granted[b] != 0;
+    held = min(a.held[b], a.cols);
+    const int rows = a.cu_rows[b + 1] - a.cu_rows[b] - kept * a.chain_len;
+    tau = min(tau, max(rows, 0));
+  }
   const bool in_range = L >= 0 && L <= a.cols * kPageTokens + kPageTokens - 1;
   const bool fills = in_range && ((L + tau) >> kPageShift) > col;
   int id = -1;
-  if (fills && col < a.cols) id = a.table[(int64_t)b * a.cols + col];
-  // no place for a block that becomes complete, or a length out of range: nothing is committed
-  const bool ok = in_range && (!fills || (uint32_t)id < (uint32_t)a.n_blocks);
+  if (fills && col < held) id = a.table[(int64_t)b * a.cols + col];
+  // refused, no place for a block that becomes complete, or a length out of range: nothing is committed
+  const bool ok = granted && in_range && (!fills || (uint32_t)id < (uint32_t)a.n_blocks);
   if (h == 0 && !values && layer == 0 && tid == 0) a.new_len[b] = ok ? L + tau : L;
   if (!ok) return;
   const int shift = kept * a.chain_len;
