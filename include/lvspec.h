@@ -359,7 +359,7 @@ typedef struct {
  * rows, n = n_new[b] rows to come (packed one request behind the other), end = len + n and
  * done = (draft ? len : end) / 64 blocks that are complete behind them:
  *     cu_rows[b]  = rows of the requests before b; cu_rows[B] = all rows (both at most max_rows)
- *     need        = (end + reserve) / 64;  grow = max(need - held[b], 0)
+ *     need        = (end + reserve) / 64 (0: finished, see below);  grow = max(need - held[b], 0)
  *     granted[b]  = need <= table_cols, the rows fit into max_rows and, open, into the ring
  *                   (end - 64 done <= 128), and (grow == 0 or the queue holds enough for the grow of all
  *                   requests up to b: first come, first served, nobody overtakes)
@@ -371,8 +371,10 @@ typedef struct {
  *         else LVSPEC_SLOT_TAIL - (128 b + p % 128); LVSPEC_SLOT_NONE for a request not granted
  *     rows cu_rows[B] .. max_rows-1: slot LVSPEC_SLOT_NONE, row_seq and row_pos -1
  * The queue is a ring int32 [n_blocks] of free blocks: state = {index of the first, number}.  At the
- * start state = {0, n_blocks}, queue = 0 .. n_blocks-1, held = 0.  A finished request is one with
- * kv_len = n_new = 0.  Nothing is changed in place but table entries at and behind held[b] and queue
+ * start state = {0, n_blocks}, queue = 0 .. n_blocks-1, held = 0.  A finished request, or a place of the
+ * batch that has none, is one with kv_len = 0 and n_new < 0: its need is 0 whatever the reserve, and all
+ * its blocks go back.  (With kv_len = n_new = 0 a request is there and empty, and is given the blocks of its
+ * reserve as any other: reserve / 64, none for less than 64 rows.)  Nothing is changed in place but table entries at and behind held[b] and queue
  * entries behind its end, so a repeated call gives the same answer.  Lengths below 0 count as 0.
  * Errors: LVSPEC_EINVAL for NULL / out-of-range arguments, new_held aliasing held or new_state state.
  * ------------------------------------------------------------------------------------------- */

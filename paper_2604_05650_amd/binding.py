@@ -592,8 +592,9 @@ def paged_plan_args(kv_len, n_new, held, queue, state, table, *, outs, max_rows,
 def paged_plan(kv_len, n_new, held, queue, state, table, *, max_rows, reserve=0, draft=False, outs=None,
                stream=None) -> dict:
     """lvspec_paged_plan.  kv_len, n_new, held int32 [B]; queue int32 [n_blocks], state int32 [2], table
-    int32 [B, cols] (queue and table are changed).  Returns granted, new_held, new_state, cu_rows, slots,
-    row_seq, row_pos; new_held and new_state are held and state of the next call."""
+    int32 [B, cols] (queue and table are changed); kv_len 0 and n_new -1 where a request has finished or
+    there is none.  Returns granted, new_held, new_state, cu_rows, slots, row_seq, row_pos; new_held and
+    new_state are held and state of the next call."""
     if outs is None:
         outs = alloc_paged_plan(table.shape[0], max_rows, table.device)
     a = paged_plan_args(kv_len, n_new, held, queue, state, table, outs=outs, max_rows=max_rows, reserve=reserve,

@@ -29,7 +29,7 @@ LVS_DEV PlanRequest plan_request(const PlanKernelArgs& a, int b) {
   r.rows = min(max(rows, 0), a.max_rows + 1);
   r.held = min(max(held, 0), a.cols);
   r.done = (a.draft ? r.len : r.len + r.rows) >> kPageShift;
-  r.need = (r.len + r.rows + a.reserve) >> kPageShift;
+  r.need = len <= 0 && rows < 0 ? 0 : (r.len + r.rows + a.reserve) >> kPageShift;      // (finished: no reserve)
   return r;
 }
 

@@ -193,3 +193,34 @@ def test_captured_steps_with_refusals(L):
     refused = [i for i, x in enumerate(seen) if 0 in x]
     assert refused and refused[-1] < 19 and min(seen[-1]) == 1
     assert kv_len.tolist()[1] == 0
+
+
+@pytest.mark.parametrize("reserve", [0, 63, 64, 80, 640])
+def test_finished_requests_hold_nothing_whatever_the_reserve(L, reserve):
+    """kv_len = 0 and n_new < 0: no block, in a place that had some and in one that had none."""
+    B, n_blocks, cols = 5, 40, 20
+    st = L.alloc_paged_state(B, n_blocks, cols, DEV)
+    planned(L, st, [0] * B, [300, 100, -1, 200, -1], 600)
+    assert st["held"].tolist() == [4, 1, 0, 3, 0]
+    table = st["table"].tolist()
+    p = planned(L, st, [0, 100, 0, -5, 0], [-1, 5, -1, -2, 0], 5, reserve=reserve)
+    assert p["granted"].tolist() == [1] * B and p["cu_rows"].tolist() == [0, 0, 5, 5, 5, 5]
+    live, empty = (105 + reserve) // T, reserve // T
+    assert st["held"].tolist() == [0, live, 0, 0, empty]
+    assert st["state"].tolist()[1] == n_blocks - live - empty
+    head, n = st["state"].tolist()
+    free = [int(st["queue"][(head + i) % n_blocks]) for i in range(n)]
+    assert free[-7:] == table[0][:4] + table[3][:3]
+    own = [x for b in range(B) for x in st["table"][b, :st["held"][b]].tolist()]
+    assert sorted(own + free) == list(range(n_blocks))
+
+
+def test_places_without_a_request_take_nothing_from_live_ones(L):
+    """First come, first served: twenty places without a request before one that needs the whole pool."""
+    B, n_blocks = 21, 10
+    st = L.alloc_paged_state(B, n_blocks, 12, DEV)
+    p = planned(L, st, [0] * B, [-1] * 20 + [64 * 8], 64 * 8, reserve=128)
+    assert p["granted"].tolist() == [1] * B and st["held"].tolist() == [0] * 20 + [10]
+    p = planned(L, st, [0] * B, [300] + [-1] * 20, 300, reserve=128)          # the first is served once it is back
+    assert p["granted"].tolist() == [0] + [1] * 20 and st["held"].tolist() == [0] * B
+    assert planned(L, st, [0] * B, [300] + [-1] * 20, 300, reserve=128)["granted"].tolist() == [1] * B
