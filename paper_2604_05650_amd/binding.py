@@ -7,6 +7,7 @@ is missing, importing this module raises.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import NamedTuple, Optional
 
@@ -236,6 +237,43 @@ def _check(status: int):
         raise LvspecError(status)
 
 
+def _tensors(x):
+    """The tensors among arguments or results (tuples, dicts)."""
+    if isinstance(x, torch.Tensor):
+        yield x
+    elif isinstance(x, (tuple, dict)):
+        for y in (x.values() if isinstance(x, dict) else x):
+            yield from _tensors(y)
+
+
+def _allocates_on_stream(call):
+    """For calls that allocate outputs or a workspace and take `stream`: they come from that stream's memory.
+    Memory of the caller's stream may still be read by work before the call, and a workspace could be
+    given out again, to a launch on a third stream, as soon as the call returns.  Results may be used (behind a
+    wait) and dropped on the caller's stream."""
+    @functools.wraps(call)
+    def on_stream(*args, stream=None, **kwargs):
+        if stream is None:
+            return call(*args, **kwargs)
+        device = next((t.device for t in _tensors((args, kwargs)) if t.is_cuda), None)
+        if device is None:                     # (refused by the call)
+            return call(*args, **kwargs)
+        caller = torch.cuda.current_stream(device)
+        handle = _stream(stream)
+        if handle == caller.cuda_stream and device.index == torch.cuda.current_device():
+            return call(*args, **kwargs)
+        if handle in (0, 1):                   # (the default stream's two names)
+            stream = torch.cuda.default_stream(device)
+        elif not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(handle, device=device)
+        with torch.cuda.stream(stream):
+            result = call(*args, **kwargs)
+        for t in _tensors(result):
+            t.record_stream(caller)
+        return result
+    return on_stream
+
+
 # What a call costs in the interpreter: new_empty of an input takes 3.6 us where torch.empty takes
 # 4.5 (outputs and workspaces of the three verify calls), one stride() 0.4 us where one per dimension
 # takes 1.5 (verify_attn_args), and an array assigned to a pointer field 0.7 us where ctypes.cast takes
@@ -275,6 +313,7 @@ def verify_attn_args(q, k, v, kv_len, *, out, vis_begin=None, vis_end=None, draf
     return a
 
 
+@_allocates_on_stream
 def verify_attn(q, k, v, kv_len, *, vis_begin=None, vis_end=None, draft_mask=None, scale=0.0,
                 out=None, return_lse=False, return_vis_mass=False, workspace=None,
                 max_kv_len=0, kv_len_host=None, stream=None):
@@ -312,6 +351,7 @@ def verify_attn_static(q, k, v, kv_len, *, out, vis_begin=None, vis_end=None, dr
     return out
 
 
+@_allocates_on_stream
 def hv_prepare(h_v, *, hv_inv_norm=None, stream=None):
     """lvspec_hv_prepare: h_v [B,lv_max,d] bf16 -> fp32 [B,lv_max] inverse row norms (once, at
     prefill), to be handed to visual_relevance at every step."""
@@ -345,6 +385,7 @@ def visual_relevance_args(h_d, h_v, l_v, top_n, *, relevance, hv_inv_norm=None) 
     return a
 
 
+@_allocates_on_stream
 def visual_relevance(h_d, h_v, l_v, top_n=10, *, relevance=None, workspace=None, stream=None,
                      hv_inv_norm=None):
     """lvspec_visual_relevance.  h_d [B,gamma,d], h_v [B,lv_max,d] bf16; l_v int32 [B] (device);
@@ -415,6 +456,7 @@ def _accept_outputs(like, B, gamma, V, topk, return_logits, return_topk, n_branc
     return outs
 
 
+@_allocates_on_stream
 def loose_accept(h_d, lm_head, draft_ids, relevance, n_loose_, pst_window, *, topk=1,
                  loose_topk_gate=0, return_logits=False, outs=None, workspace=None, stream=None,
                  n_branches=1, return_entropy=False, bonus_row=False, rule=RULE_VISUAL,
@@ -446,6 +488,7 @@ def loose_accept(h_d, lm_head, draft_ids, relevance, n_loose_, pst_window, *, to
     return outs
 
 
+@_allocates_on_stream
 def kv_commit(k, v, kv_len, accept_len, chain_len, *, best_branch=None, n_branches=1, new_len=None,
               stream=None):
     """lvspec_kv_commit.  k, v bf16 [B,Hkv,cap,D] or [layers,B,Hkv,cap,D] (changed in place),
@@ -589,6 +632,7 @@ def paged_plan_args(kv_len, n_new, held, queue, state, table, *, outs, max_rows,
     return a
 
 
+@_allocates_on_stream
 def paged_plan(kv_len, n_new, held, queue, state, table, *, max_rows, reserve=0, draft=False, outs=None,
                stream=None) -> dict:
     """lvspec_paged_plan.  kv_len, n_new, held int32 [B]; queue int32 [n_blocks], state int32 [2], table
@@ -653,6 +697,7 @@ def verify_attn_paged_args(q, cache: PagedCache, table, kv_len, *, out, vis_begi
     return a
 
 
+@_allocates_on_stream
 def verify_attn_paged(q, cache: PagedCache, table, kv_len, *, vis_begin=None, vis_end=None, draft_mask=None,
                       scale=0.0, out=None, return_lse=False, return_vis_mass=False, workspace=None,
                       stream=None):
@@ -692,6 +737,7 @@ def paged_commit_args(cache: PagedCache, table, kv_len, accept_len, chain_len, *
     return a
 
 
+@_allocates_on_stream
 def paged_commit(cache: PagedCache, table, kv_len, accept_len, chain_len, *, best_branch=None, n_branches=1,
                  new_len=None, plan=None, stream=None):
     """lvspec_paged_commit.  cache of one layer, or of all with a leading dimension; accept_len int32
