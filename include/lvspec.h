@@ -318,8 +318,9 @@ int lvspec_kv_commit(const lvspec_commit_args* args, void* stream);
  *   v_pool   e4m3 [n_blocks, Hkv, 128, 64]     values of a complete block, a channel per row
  *   k_scale, v_scale   fp32 [n_blocks, Hkv]    value = code * scale; the scale is the smallest power of
  *                                              two s >= 2^-60 with max |x| <= 448 s over the block's
- *                                              finite values; codes are rounded to nearest even, what
- *                                              is not finite becomes NaN
+ *                                              finite values; codes are rounded to nearest even (at
+ *                                              s = 2^120 to 240 at most, whose value binary32 holds),
+ *                                              what is not finite becomes NaN
  *   k_tail, v_tail     bf16 [B, Hkv, 128, 128] ring of LVSPEC_TAIL_ROWS rows per sequence: position p at
  *                                              row p % 128
  * and, shared by the layers, a table int32 [B, table_cols]: entry j is the block of positions 64 j ..

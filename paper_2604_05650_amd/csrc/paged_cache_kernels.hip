@@ -207,9 +207,17 @@ LVS_DEV uint32_t pack_fp8(float a, float b, float c, float d) {
   return (uint32_t)r;
 }
 
+// Magnitudes from 248 * 2^120 on, the last ones of bf16, to 240 * 2^120: the nearest code would be 256, whose value
+// at the scale of 2^120 is 2^128, beyond bf16 and binary32.  What is not finite stays.
+constexpr uint32_t kTopCode = 0x7f70, kBeyond = 0x7f78;      // bits of 240 and 248 * 2^120
+LVS_DEV uint32_t below_top(uint32_t x) {
+  const uint32_t m = x & 0x7fffu;
+  return m > kTopCode && m < 0x7f80u ? (x & 0x8000u) | kTopCode : x;
+}
+
 // x[i]: this thread's chunk of row 4q + i.  The scale is a power of two: x * 2^-e is exact, the conversion
 // is the only rounding.  Every thread of the workgroup takes part.
-LVS_DEV void store_block(const u32x4 (&x)[4], bool turned, uint8_t* dst, float* scale, uint32_t* s_turn,
+LVS_DEV void store_block(u32x4 (&x)[4], bool turned, uint8_t* dst, float* scale, uint32_t* s_turn,
                          uint32_t* s_max) {
   const int tid = threadIdx.x, q = tid >> 4, c = tid & 15;
   uint32_t amax = 0;
@@ -225,6 +233,12 @@ LVS_DEV void store_block(const u32x4 (&x)[4], bool turned, uint8_t* dst, float* 
   if ((tid & 63) == 0) s_max[tid >> 6] = amax;
   __syncthreads();
   amax = max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3]));
+  if (amax >= kBeyond) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[i][j] = below_top(x[i][j] & 0xffffu) | below_top(x[i][j] >> 16) << 16;
+  }
   const int e = scale_exponent(amax);
   const float inv = __builtin_bit_cast(float, (uint32_t)(127 - e) << 23);
   if (tid == 0) *scale = __builtin_bit_cast(float, (uint32_t)(127 + e) << 23);

@@ -1,0 +1,74 @@
+"""The paged cache at the ends of bf16's range.  Codes and scales are equal to the plain form's."""
+import numpy as np
+import pytest
+import torch
+
+import paged_ref as R
+from test_gpu_paged import D, DEV, L, RING, T, i32, normal, ready, same_cache  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+MOST = float(torch.finfo(torch.bfloat16).max)
+
+
+def finite_block(x):
+    """block8 with codes of finite values that have finite values: 240 at most at the scale 2^120."""
+    _, s = R.block8(x)
+    top = 240.0 if s == 2.0 ** 120 else 448.0
+    return R.nearest8(np.where(np.isfinite(x), np.clip(x / s, -top, top), x)), s
+
+
+def extreme_rows(seed):
+    """Three blocks: the largest values, ones around 248 * 2^120 with others of every size, and 247 * 2^120."""
+    x = torch.randn(3, T, D, generator=torch.Generator().manual_seed(seed)) * 2.0 ** 118
+    x[0, ::3] = MOST
+    x[0, 1::3] = -MOST
+    x[0, 5, 7], x[0, 6, 7], x[0, 7, 7] = float("inf"), float("-inf"), float("nan")
+    x[1, 2, 3], x[1, 2, 4], x[1, 9, 9] = 248.0 * 2.0 ** 120, -247.0 * 2.0 ** 120, 225.0 * 2.0 ** 120
+    x[1, 20:] = torch.randn(T - 20, D, generator=torch.Generator().manual_seed(seed + 1))
+    x[2, 4, 4] = -247.0 * 2.0 ** 120
+    return x.to(torch.bfloat16)
+
+
+@pytest.mark.parametrize("by", ["append", "commit"])
+def test_largest_values_stay_finite(L, by):  # noqa: F811
+    H, rows = 2, torch.stack([extreme_rows(1), extreme_rows(5)], 2)           # [3, T, H, D]
+    if by == "append":
+        cache = L.alloc_paged_cache(1, H, 3, DEV)
+        st = L.alloc_paged_state(1, 3, 3, DEV)
+        k = rows.reshape(3 * T, H, D).to(DEV)
+        v = rows.flip(1).reshape(3 * T, H, D).contiguous().to(DEV)
+        plan = L.paged_plan(i32([0]), i32([3 * T]), st["held"], st["queue"], st["state"], st["table"], max_rows=3 * T)
+        L.paged_append(cache, k, v, plan)
+        ids = st["table"][0].tolist()
+    else:                                                                    # the last row of three sequences' blocks
+        cache, ids = L.alloc_paged_cache(3, H, 3, DEV), [2, 0, 1]
+        cache.k_tail[:, :, :T] = rows.transpose(1, 2).to(DEV)
+        cache.v_tail[:, :, :T] = rows.flip(1).transpose(1, 2).to(DEV)
+        assert L.paged_commit(cache, i32([[i] for i in ids]), i32([T - 1] * 3), i32([1] * 3), 1).tolist() == [T] * 3
+    k8, v8, ks, vs = R.as_numpy(cache)[:4]
+    for j, i in enumerate(ids):
+        for h in range(H):
+            for pool, scale, x in ((k8, ks, rows[j, :, h]), (v8, vs, rows[j].flip(0)[:, h])):
+                x = x.double().numpy()
+                got = pool[i, h] if pool is k8 else pool[i, h].T
+                codes, s = finite_block(x)
+                nan = ~np.isfinite(x)
+                assert scale[i, h] == s and np.array_equal(got[~nan], codes[~nan]) and np.all(got[nan] & 127 == 127)
+                value = (R.value_of(got[~nan]) * s).astype(np.float32)
+                assert np.all(np.isfinite(value)) and np.all(np.abs(value - x[~nan]) <= np.abs(x[~nan]) * 2.0 ** -4 + s * 2.0 ** -10)
+    assert ks.max() == 2.0 ** 120
+
+
+def test_attention_over_the_largest_values(L):  # noqa: F811
+    """Equal weights over one block of the largest values: their mean is finite, where one infinite value would
+    not be."""
+    cache = L.alloc_paged_cache(1, 1, 1, DEV)
+    rows = torch.full((T, 1, D), MOST, dtype=torch.bfloat16, device=DEV)
+    rows[1::2] = -MOST
+    st = L.alloc_paged_state(1, 1, 1, DEV)
+    plan = L.paged_plan(i32([0]), i32([T]), st["held"], st["queue"], st["state"], st["table"], max_rows=T)
+    L.paged_append(cache, torch.zeros_like(rows), rows, plan)
+    out = L.verify_attn_paged(torch.ones((1, 1, 1, D), dtype=torch.bfloat16, device=DEV), cache, st["table"], i32([T]))
+    # 65 keys of score 0, the draft row's value 0
+    assert bool((out.abs() <= 2.0 ** 128 * 1e-6).all())
