@@ -31,7 +31,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kMergeStride = 132;      // floats per row in the merge buffer: output and two sums
-constexpr float kNegBig = -1.0e30f;
+constexpr float kNegBig = -3.4028234663852886e38f;      // below every finite score: a maximum of nothing, with no inf - inf
 constexpr uint32_t kBufferWord = 0x00020000;      // last word of a buffer resource: raw, 32-bit data
 
 // eight e4m3 times 2^e as bf16 (exact)

@@ -72,3 +72,42 @@ def test_attention_over_the_largest_values(L):  # noqa: F811
     out = L.verify_attn_paged(torch.ones((1, 1, 1, D), dtype=torch.bfloat16, device=DEV), cache, st["table"], i32([T]))
     # 65 keys of score 0, the draft row's value 0
     assert bool((out.abs() <= 2.0 ** 128 * 1e-6).all())
+
+
+@pytest.mark.parametrize("spare_cols", [1, 70])        # a unit in one workgroup, or cut into parts
+@pytest.mark.parametrize("rows", [1, 40])              # query rows of a kv head: 16x16 and 32x32 cores
+@pytest.mark.parametrize("n", [0, 3, 64, 1500])
+def test_scores_far_below_any_usual_one(L, n, rows, spare_cols):  # noqa: F811
+    """All scores of a row near -2^110 (-1.3e33), exact powers of two that differ by far more than any softmax
+    resolves: the row is the value of its largest score, equal ones share it, and lse is that score."""
+    H, g = 2, 1
+    cache, table = ready(L, 900 + n, 1, H, [n], spare_cols=spare_cols)
+    # keys: channel 3 alone is not zero, code 2^-6 .. 2^0 with scale 2^0 in blocks, the same in the ring
+    rng = np.random.default_rng(n)
+    size = torch.from_numpy(2.0 ** -rng.integers(0, 4, (H, n + g))).float()
+    value = torch.from_numpy(rng.integers(-8, 9, (H, n + g, D)) / 4.0).float()
+    k8, v8 = torch.zeros(cache.k_pool.shape), torch.zeros(cache.v_pool.shape)
+    for j in range(n // T):
+        for h in range(H):
+            k8[table[0, j], h, :, 3] = size[h, j * T:j * T + T]
+            v8[table[0, j], h] = value[h, j * T:j * T + T].T
+    cache.k_pool.copy_(k8.to(torch.float8_e4m3fn))
+    cache.v_pool.copy_(v8.to(torch.float8_e4m3fn))
+    cache.k_scale.fill_(1.0)
+    cache.v_scale.fill_(1.0)
+    cache.k_tail.zero_()
+    for p in range(n // T * T, n + g):
+        cache.k_tail[0, :, p % RING, 3] = size[:, p].to(DEV, torch.bfloat16)
+        cache.v_tail[0, :, p % RING] = value[:, p].to(DEV, torch.bfloat16)
+    q = torch.zeros((1, g, rows * H, D))
+    q[..., 3] = -2.0 ** 113
+    out, lse, _ = L.verify_attn_paged(q.to(DEV, torch.bfloat16), cache, i32(table), i32([n]), scale=1.0, return_lse=True)
+    for h in range(H):
+        least = float(size[h].min())
+        equal = size[h] == least
+        want = value[h][equal].double().mean(0)
+        got = out[0, 0, h * rows:(h + 1) * rows].double().cpu()
+        # the weights are 1 and 0; values are multiples of 1/4: the sum is exact, 1/l and the product 2^-23, out 2^-8
+        assert bool(((got - want).abs() <= (2.0 ** -8 + 2.0 ** -22) * want.abs() + 1e-30).all())
+        s = lse[0, h * rows:(h + 1) * rows].double().cpu()
+        assert bool(((s + 2.0 ** 113 * least).abs() <= 2.0 ** 113 * least * 2.0 ** -21).all())
