@@ -600,6 +600,16 @@ def _call_on(device, fn, a, stream):
             _check(fn(C.byref(a), _stream(stream)))
 
 
+def _strides(t):
+    """Strides of all but the last dimension.  torch gives any stride to a dimension of one: a row's."""
+    return [s if n > 1 else 128 for n, s in zip(t.shape[:-1], t.stride())]
+
+
+def _strides(t):
+    """Strides of all but the last dimension.  torch gives any stride to a dimension of one: a row's."""
+    return [s if n > 1 else 128 for n, s in zip(t.shape[:-1], t.stride())]
+
+
 def _cache_struct(cache: PagedCache, lead=()) -> PagedCacheStruct:
     n = len(lead)
     n_blocks, Hkv = cache.k_pool.shape[n:n + 2]
@@ -656,9 +666,7 @@ def paged_append_args(cache: PagedCache, k, v, plan) -> PagedAppendArgs:
     assert k.is_cuda and v.is_cuda and k.dtype == torch.bfloat16 and v.dtype == torch.bfloat16 and k.shape == v.shape
     assert k.shape[1:] == (a.cache.Hkv, 128) and k.stride(-1) == 1 and v.stride(-1) == 1
     a.n_rows, a.k, a.v = n, k.data_ptr(), v.data_ptr()
-    # (torch gives any stride to a dimension of one)
-    a.k_sr, a.k_sh, a.v_sr, a.v_sh = [x.stride(d) if x.shape[d] > 1 else max(x.stride(d), 128)
-                                      for x in (k, v) for d in (0, 1)]
+    (a.k_sr, a.k_sh), (a.v_sr, a.v_sh) = _strides(k), _strides(v)
     a.slots, a.row_seq, a.row_pos = (_dense(plan[x], i32, (n,)) for x in ("slots", "row_seq", "row_pos"))
     a.cu_rows = _dense(plan["cu_rows"], i32, (a.cache.B + 1,))
     return a
@@ -682,7 +690,7 @@ def verify_attn_paged_args(q, cache: PagedCache, table, kv_len, *, out, vis_begi
     assert out.shape == q.shape
     assert B == a.cache.B and D == 128 and q.stride(-1) == 1 and out.stride(-1) == 1
     a.gamma, a.Hq = gamma, Hq
-    a.q, (a.q_sb, a.q_sg, a.q_sh) = q.data_ptr(), q.stride()[:3]
+    a.q, (a.q_sb, a.q_sg, a.q_sh) = q.data_ptr(), _strides(q)
     a.table, a.table_cols = _dense(table, i32, (B, table.shape[1])), table.shape[1]
     a.kv_len = _dense(kv_len, i32, (B,))
     for name, t in (("vis_begin", vis_begin), ("vis_end", vis_end)):
@@ -691,7 +699,7 @@ def verify_attn_paged_args(q, cache: PagedCache, table, kv_len, *, out, vis_begi
         assert len(draft_mask) == gamma
         a._keep = a.draft_mask = (C.c_uint32 * gamma)(*[int(m) for m in draft_mask])
     a.scale = float(scale)
-    a.out, (a.o_sb, a.o_sg, a.o_sh) = out.data_ptr(), out.stride()[:3]
+    a.out, (a.o_sb, a.o_sg, a.o_sh) = out.data_ptr(), _strides(out)
     for name, t in (("lse", lse), ("vis_mass", vis_mass)):
         setattr(a, name, None if t is None else _dense(t, torch.float32, (B, Hq, gamma)))
     return a

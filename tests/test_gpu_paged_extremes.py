@@ -111,3 +111,20 @@ def test_scores_far_below_any_usual_one(L, n, rows, spare_cols):  # noqa: F811
         assert bool(((got - want).abs() <= (2.0 ** -8 + 2.0 ** -22) * want.abs() + 1e-30).all())
         s = lse[0, h * rows:(h + 1) * rows].double().cpu()
         assert bool(((s + 2.0 ** 113 * least).abs() <= 2.0 ** 113 * least * 2.0 ** -21).all())
+
+
+def test_strides_of_dimensions_of_one(L):  # noqa: F811
+    """torch gives a dimension of one any stride, as a view with a swapped dimension has: no call goes by it."""
+    cache, table = ready(L, 950, 1, 1, [100])
+    q, t, n = normal(951, (1, 1, 1, D)), i32(table), i32([100])
+    want = L.verify_attn_paged(q, cache, t, n)
+    for strides in ((1, 1, 1, 1), (0, 0, 0, 1), (4, 2, 7, 1), (D, D, 1, 1)):
+        odd = q.as_strided((1, 1, 1, D), strides)
+        out = torch.zeros_like(want).as_strided((1, 1, 1, D), strides)
+        assert torch.equal(L.verify_attn_paged(odd, cache, t, n, out=out), want) and torch.equal(out, want)
+    rows = normal(952, (1, 1, D))
+    maps = dict(slots=i32([-2 - 100]), row_seq=i32([0]), row_pos=i32([100]), cu_rows=i32([0, 1]))
+    for strides in ((1, 1, 1), (0, 0, 1), (129, 131, 1)):
+        cache.k_tail.zero_()
+        L.paged_append(cache, rows.as_strided((1, 1, D), strides), rows, maps)
+        assert torch.equal(cache.k_tail[0, 0, 100], rows[0, 0])
