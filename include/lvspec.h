@@ -432,6 +432,10 @@ int lvspec_paged_append(const lvspec_paged_append_args* args, void* stream);
  * table entry below L / 64 that names no block of the pool holds no key: its positions are left out.
  * Where a sequence's keys are cut, and with that the rounding of its bf16 probabilities (a relative 2e-3
  * of the result), follows from the lengths of all sequences and the shapes.
+ * table_cols says how the call is launched: at most 18 columns (64 where B * Hkv * ceil(gamma * Hq / Hkv / 32) is
+ * half the compute units or more) go in one kernel, which short contexts want (777 keys: 7.8 us, and 9.8 with
+ * 1024 columns); wider tables are cut along the keys and merged by a second kernel, up to 256 sequences.  More
+ * sequences are not cut: there one far longer than the others takes as long as a few compute units read it.
  * Errors: as lvspec_verify_attn; LVSPEC_EUNSUPPORTED for more than 2^21 units, a unit being 32 rows or the rest
  * of a sequence's kv head, and for more than 2^30 units times (table_cols + 8) or rows of all kv heads.
  * ------------------------------------------------------------------------------------------- */

@@ -10,8 +10,8 @@
 //             operand, and probabilities stay in their lane.
 //   The conversion multiplies by the block's scale (a power of two): exact, and nothing is left to scale.
 //   Softmax in base 2 with a running maximum, sums in 32 bits; probabilities are rounded to bf16 for the
-//   second product (relative 2^-9 each, which averages out over the keys; it is what the matrix
-//   instructions take).  Open rows, at most 95 in bf16, are taken 32 at a time by the streams of a unit's first
+//   second product (each by at most 2^-8 of itself, 2^-9 on average, which averages out over the keys; it is what the
+//   matrix instructions take).  Open rows, at most 95 in bf16, are taken 32 at a time by the streams of a unit's first
 //   part.  The streams merge through LDS in fixed order into one record per part.
 // Kernel 2 (combine): merge of a row's records in fixed order, bf16 output.
 // Small tables: one workgroup per unit writes the output itself, and there is no second kernel.
@@ -788,7 +788,7 @@ LVS_DEV float* record_at(const PagedAttnKernelArgs& p, int64_t i) { return p.ws 
 LVS_DEV int2* records_of(const PagedAttnKernelArgs& p) { return reinterpret_cast<int2*>(record_at(p, p.limit)); }
 
 // All cache lines of a kernel's arguments at its start, not one miss behind the other: 16384 keys, 25 rows 15.9 us
-// without and 15.6, 100 rows 22.7 and 22.4, 777 keys 8.1 and 7.9.
+// without and 15.6, 100 rows 22.7 and 22.4 (four streams), 777 keys 8.1 and 7.9.
 LVS_DEV void ask_for_arguments(const PagedAttnKernelArgs& p) {
   asm volatile("" ::"s"(p.q), "s"(p.k8), "s"(p.table), "s"(p.G), "s"(p.vis_begin), "s"(p.out), "s"(p.ws));
 }
@@ -942,8 +942,11 @@ __global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(PagedAtt
 // have as many blocks, so the more units there are, the more of them pay: they fill the chip anyway.  One
 // workgroup per unit and parts, us: 8 units 800 keys 11.1 and 12.4, 1100 12.2 and 12.7, 1400 13.9 and 12.7;
 // 64 units 1000 keys 13.3 and 13.8, 1500 15.9 and 14.4; 128 units 2000 keys 18.6 and 20.7, 3000 24.6 and 26.1;
-// 256 units 4000 keys 45.9 and 49.8, 512 units 91.6 and 89.6.  More than 64 kPer sequences are not cut, whose places
-// a wave cannot hold: 250 x (400 to 12000) keys, 2 heads 96 and 92.
+// 256 units 4000 keys 45.9 and 49.8, 512 units 91.6 and 89.6.  It goes by the table's width, not by the lengths, which
+// the host does not know: 777 keys, 2 heads 7.8 us with 13 columns, 9.8 with 1024.
+// More than 64 kPer sequences are not cut, whose places a wave cannot hold.  That costs little where lengths are alike,
+// 250 x (400 to 12000) keys, 2 heads 96 and 92, and much where one sequence is far longer than the others: one of
+// 65536 keys among 500 each, 8 heads, 1 row of 5 heads 176 us with 256 sequences and 308 with 257.
 int unit_columns(int64_t B, int64_t units, int64_t cus) {
   return B > 64 * kPer ? 1 << 30 : units >= cus / 2 ? 64 : 18;
 }
@@ -990,9 +993,10 @@ hipError_t launch_paged_attn(const PagedAttnKernelArgs& a, hipStream_t stream) {
   }
   // More than 64 rows are bound by vector instructions, beside which the matrix unit has more to do with two waves on a
   // SIMD.  But then one workgroup fills a CU, and parts beyond the compute units wait for a second turn: that
-  // is for few units only.  Four and eight streams, us: 16384 keys, 100 rows 22.8 and 21.4; 2 x 16000, 150 rows 40.6 and
-  // 36.8; 5 x (1000 to 20000), 100 rows, 160 units 38.0 and 36.1; 6 of them, 192 units 47.7 and 54.3; 64 rows 12 x
-  // (1000 to 20000) 54.4 and 59.7; 25 rows, 16384 keys 16.0 and 16.9.
+  // is for few units only.  Four and eight streams, us: 16384 keys, 100 rows 22.5 and 22.2 (24.5 both from memory rather
+  // than the cache before it); 32000 keys, 100 rows 32.7 and 31.8; 60000 keys, 150 rows 68 and 63; 2 x 16000, 150 rows
+  // 40.6 and 38.4; 5 x (1000 to 20000), 100 rows, 160 units 37.8 and 36.7; 6 of them, 192 units 47.7 and 54.3; 64 rows
+  // 12 x (1000 to 20000) 54.4 and 59.7; 25 rows, 16384 keys 16.0 and 16.9.
   if (a.n_rc >= 3 && units * 8 <= cus * 5) return launch_parts<WideRows, 8, false>(a, stream);
   if (a.rpad <= 16) return launch_parts<Rows16, 4, true>(a, stream);
   return once ? launch_parts<WideRows, 4, true>(a, stream) : launch_parts<WideRows, 4, false>(a, stream);
