@@ -365,8 +365,11 @@ __global__ __launch_bounds__(kCacheThreads) void paged_append_kernel(AppendKerne
 // of the draft area, and the block that they complete goes into the pool.  Both read the rows where the step
 // left them; what is written (rows L .. L+tau-1, and the pool) is read by neither.
 // All layers in one launch: a layer alone would be mostly launch.  Bound by memory where blocks become complete:
-// 64 layers, 8 heads, 1 sequence 7.5 us for 25 MB, of which 3 are launch and lengths; 16 sequences with two
+// 64 layers, 8 heads, 1 sequence 7.2 us for 25 MB, of which 3 are launch and lengths; 16 sequences with two
 // chains of 10, a quarter of them with a block, 27 us for 126 MB, 4.6 TB/s.
+// PLANNED: with what the step's plan granted, in a kernel of its own, whose loads go out with the lengths': 7.3 and
+// 27.6 us per call, without a plan 7.2 and 27.3; chosen in one kernel 8.0 and 28.4.
+template <bool PLANNED>
 __global__ __launch_bounds__(kCacheThreads) void paged_commit_kernel(PagedCommitKernelArgs a) {
   __shared__ __align__(16) uint32_t s_turn[kTurnDwords];
   __shared__ uint32_t s_max[4];
@@ -375,27 +378,26 @@ __global__ __launch_bounds__(kCacheThreads) void paged_commit_kernel(PagedCommit
   const bool values = blockIdx.y != 0;
   const int64_t layer = blockIdx.z;
   const int L = a.kv_len[b];
+  // The table keeps entries of blocks that were given back, so what a sequence has is told by the plan: rows that
+  // were not granted are not in the ring, and a block behind the held ones is another sequence's.
+  int granted = 1, held = a.cols, rows = 0;
+  if constexpr (PLANNED) {
+    granted = a.granted[b];
+    held = min(a.held[b], a.cols);
+    rows = a.cu_rows[b + 1] - a.cu_rows[b];
+  }
   int kept = a.best_branch != nullptr ? a.best_branch[b] : 0;
   kept = kept < 0 || kept >= a.n_branches ? 0 : kept;
   int tau = a.accept_len[b * a.n_branches + kept];
   tau = tau < 0 ? 0 : tau > a.chain_len ? a.chain_len : tau;
+  if constexpr (PLANNED) tau = max(min(tau, rows - kept * a.chain_len), 0);
   const int col = L >> kPageShift;
-  // The table keeps entries of blocks that were given back, so what a sequence has is told by the plan: rows that
-  // were not granted are not in the ring, and a block behind the held ones is another sequence's.
-  bool granted = true;
-  int held = a.cols;
-  if (a.granted != nullptr) {
-    granted = a.granted[b] != 0;
-    held = min(a.held[b], a.cols);
-    const int rows = a.cu_rows[b + 1] - a.cu_rows[b] - kept * a.chain_len;
-    tau = min(tau, max(rows, 0));
-  }
   const bool in_range = L >= 0 && L <= a.cols * kPageTokens + kPageTokens - 1;
   const bool fills = in_range && ((L + tau) >> kPageShift) > col;
   int id = -1;
   if (fills && col < held) id = a.table[(int64_t)b * a.cols + col];
   // refused, no place for a block that becomes complete, or a length out of range: nothing is committed
-  const bool ok = granted && in_range && (!fills || (uint32_t)id < (uint32_t)a.n_blocks);
+  const bool ok = granted != 0 && in_range && (!fills || (uint32_t)id < (uint32_t)a.n_blocks);
   if (h == 0 && !values && layer == 0 && tid == 0) a.new_len[b] = ok ? L + tau : L;
   if (!ok) return;
   const int shift = kept * a.chain_len;
@@ -437,7 +439,10 @@ hipError_t launch_paged_append(const AppendKernelArgs& a, hipStream_t stream) {
 
 hipError_t launch_paged_commit(const PagedCommitKernelArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)(a.B * a.Hkv), 2, (unsigned)a.n_layers);
-  paged_commit_kernel<<<grid, dim3(kCacheThreads), 0, stream>>>(a);
+  if (a.granted != nullptr)
+    paged_commit_kernel<true><<<grid, dim3(kCacheThreads), 0, stream>>>(a);
+  else
+    paged_commit_kernel<false><<<grid, dim3(kCacheThreads), 0, stream>>>(a);
   return hipGetLastError();
 }
 
