@@ -459,10 +459,10 @@ def _calls(s):
             opt = dict(vis_begin=s["vis"][0], vis_end=s["vis"][1])
         if c["branches"] > 1:
             opt["draft_mask"] = s["mask"]
-        a = L.verify_attn_paged4_args(s["q"], L.Paged4Cache(*s["cache"]), s["table"], s["kv_len"], out=out, **opt, **more)
-        space = torch.empty((lib.lvspec_verify_attn_paged4_workspace(C.byref(a)),), dtype=torch.uint8, device=DEV)
+        a = L.verify_attn_paged_mx_args(s["q"], L.PagedMxCache(*s["cache"]), s["table"], s["kv_len"], out=out, **opt, **more)
+        space = torch.empty((lib.lvspec_verify_attn_paged_mx_workspace(C.byref(a)),), dtype=torch.uint8, device=DEV)
         a.workspace, a.workspace_bytes = space.data_ptr(), space.numel()
-        return [(lib.lvspec_verify_attn_paged4, a)], dict(more, out=out), space
+        return [(lib.lvspec_verify_attn_paged_mx, a)], dict(more, out=out), space
     rot = L.Rotary(s["inv_freq"], axis=s["axis"], interleaved=c["interleaved"], factor=c.get("factor", 1.0))
     q = None if s["q"] is None else torch.empty_like(s["q"])
     if c["kind"] == "rotary":
@@ -473,11 +473,11 @@ def _calls(s):
     if c["kind"] == "append":
         a = L.paged_append_rotary_args(L.PagedCache(*s["cache"]), s["k"], s["v"], s, rot, pos=s["pos"], q=s["q"], q_out=q)
         return [(lib.lvspec_paged_append_rotary, a)], outs, None
-    cache = L.Paged4Cache(*s["cache"])
+    cache = L.PagedMxCache(*s["cache"])
     back = {x: torch.empty((len(s["back"]), c["Hkv"], 128), dtype=torch.bfloat16, device=DEV) for x in ("k_back", "v_back")}
-    a = L.paged4_append_args(cache, s["k"], s["v"], s, rot=rot, pos=s["pos"], q=s["q"], q_out=q)
-    b = L.paged4_read_args(cache, s["back"], k=back["k_back"], v=back["v_back"])
-    return [(lib.lvspec_paged4_append, a), (lib.lvspec_paged4_read, b)], dict(outs, **back), None
+    a = L.paged_mx_append_args(cache, s["k"], s["v"], s, rot=rot, pos=s["pos"], q=s["q"], q_out=q)
+    b = L.paged_mx_read_args(cache, s["back"], k=back["k_back"], v=back["v_back"])
+    return [(lib.lvspec_paged_mx_append, a), (lib.lvspec_paged_mx_read, b)], dict(outs, **back), None
 
 
 def run(s):
