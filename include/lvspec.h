@@ -496,6 +496,195 @@ typedef struct {
 int lvspec_paged_commit(const lvspec_paged_commit_args* args, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Rotary positions (beyond the paper, whose models bring their own): query and key rows turned by their
+ * positions before they meet.  With i < dim / 2, t a row, D its channels and the others left as they are:
+ *     a = pos[axis[i], t] * inv_freq[i]         c = factor cos a      s = factor sin a
+ *     y1 = x1 c - x2 s,  y2 = x2 c + x1 s       (x1, x2): channels i, i + dim/2, interleaved 2 i, 2 i + 1
+ * transpose = 1 turns back (s negative), the gradient of x from that of y.  A token of a video has a position
+ * on several axes (time, height, width), and a frequency goes by one of them.  Angles, their cosines and
+ * sines, and the two products are in 64 bits; the result is rounded to binary32 and then to the rows' type.
+ * Where frequencies are stretched for long contexts, inv_freq and factor say how (lvspec_rotary_frequencies).
+ * Rows may be turned in place (out = in, with the same strides) and must not overlap otherwise.
+ * Errors: LVSPEC_EINVAL for NULL / misaligned / out-of-range arguments, LVSPEC_EUNSUPPORTED for D > 512, more than
+ * 65535 heads or 2^32 row channels (n_rows * D).
+ * ------------------------------------------------------------------------------------------- */
+enum { LVSPEC_BF16 = 0, LVSPEC_F16 = 1, LVSPEC_F32 = 2 };
+
+typedef struct {
+  int32_t dim;                      /* channels that are turned, the first of every head; even, >= 2 */
+  int32_t interleaved;              /* 0: halves, 1: neighbours */
+  int32_t transpose;                /* 0 or 1 */
+  int32_t n_axes;                   /* 1 .. 4 */
+  const float* inv_freq;            /* DEVICE [dim / 2] */
+  const uint8_t* axis;              /* DEVICE [dim / 2], each below n_axes (else the last); NULL: the first */
+  const int32_t* pos;               /* DEVICE [n_axes, n_rows] */
+  int64_t pos_sa;                   /* stride of pos: axis */
+  float factor;                     /* of cosines and sines, > 0; 0 = 1 */
+} lvspec_rotation;
+
+typedef struct {
+  lvspec_rotation rot;
+  int32_t n_rows, Hq, Hkv, D;       /* Hq >= 1; Hkv = 0: no second tensor; dim <= D <= 512 */
+  int32_t dtype;                    /* LVSPEC_BF16, _F16 or _F32: of all rows */
+  const void* q;                    /* DEVICE [n_rows, Hq, D] */
+  int64_t q_sr, q_sh;               /* strides: row, head */
+  void* q_out;                      /* DEVICE, as q */
+  int64_t qo_sr, qo_sh;
+  const void* k;                    /* DEVICE [n_rows, Hkv, D], by the same positions */
+  int64_t k_sr, k_sh;
+  void* k_out;
+  int64_t ko_sr, ko_sh;
+} lvspec_rotary_args;
+
+int lvspec_rotary(const lvspec_rotary_args* args, void* stream);
+
+/* Frequencies on the host, in binary64 and rounded once.  f_i = base^(-2 i / dim):
+ *   LVSPEC_SCALING_NONE     f_i
+ *   LVSPEC_SCALING_LINEAR   f_i / scale                            (positions squeezed)
+ *   LVSPEC_SCALING_NTK      f_i with base * scale^(dim / (dim - 2))      (the last as LINEAR, the first as NONE)
+ *   LVSPEC_SCALING_YARN     f_i (1 - r_i) + f_i / scale r_i,  r_i = clamp((i - low) / (high - low), 0, 1) with low and
+ *                           high the frequencies, floor and ceiling within [0, dim - 1], that turn beta_fast and
+ *                           beta_slow times over original_len; factor = 0.1 ln(scale) + 1 for scale > 1
+ * and factor = 1 otherwise. */
+enum { LVSPEC_SCALING_NONE = 0, LVSPEC_SCALING_LINEAR = 1, LVSPEC_SCALING_NTK = 2, LVSPEC_SCALING_YARN = 3 };
+
+typedef struct {
+  int32_t dim;                      /* even, 2 .. 512; > 2 for LVSPEC_SCALING_NTK */
+  int32_t scaling;
+  double base;                      /* > 1 */
+  double scale;                     /* > 0; unused without scaling */
+  double original_len;              /* LVSPEC_SCALING_YARN: positions of the context before it was stretched, > 0 */
+  double beta_fast, beta_slow;      /* 0 = 32 and 1; fast >= slow > 0 */
+} lvspec_rotary_freq_args;
+
+int lvspec_rotary_frequencies(const lvspec_rotary_freq_args* args, float* inv_freq /* HOST [dim / 2] */,
+                              float* factor /* HOST */);
+
+/* ---------------------------------------------------------------------------------------------
+ * lvspec_paged_append with the keys rotated on the way, and the rows' queries beside them in the same launch.  A
+ * rotated key is rounded to bf16, as the ring holds it, before its block is rounded to 8 bits.  pos = NULL: rows are
+ * turned by rows.row_pos, their places in the cache (n_axes 1).  Rows with row_seq < 0 have no query: theirs is left
+ * as it is in q_out.
+ * Errors: as lvspec_paged_append and lvspec_rotary; LVSPEC_EUNSUPPORTED for dim % 16 != 0, and for more than 2^24
+ * workgroups, n_rows * Hkv / 32 + n_rows / 32; LVSPEC_EINVAL for transpose.
+ * ------------------------------------------------------------------------------------------- */
+typedef struct {
+  lvspec_paged_append_args rows;    /* k not rotated yet */
+  lvspec_rotation rot;
+  int32_t Hq;                       /* 0: no queries */
+  const void* q;                    /* DEVICE bf16 [n_rows, Hq, 128] */
+  int64_t q_sr, q_sh;
+  void* q_out;                      /* DEVICE, as q */
+  int64_t qo_sr, qo_sh;
+} lvspec_paged_append_rotary_args;
+
+int lvspec_paged_append_rotary(const lvspec_paged_append_rotary_args* args, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Paged KV cache in 4 bits, in groups of 32 with a scale ("mx"): as the one in 8 bits, by the same plans, tables, slots and rings, with a complete block
+ * in 8704 bytes a kv head instead of 16392.  Codes are e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign) and 32 values
+ * share a scale, a power of two held as its exponent + 127 in a byte: of a key 32 channels of a token, of the values
+ * 32 tokens of a channel.  value = code * scale; the scale is the smallest power of two s >= 2^-60 with max |x| <= 7 s,
+ * so that no value is further from its code's than half a step there (codes end at 6, the next would be 8); codes
+ * are rounded to nearest even (at s = 2^126 to 3 at most, whose value binary32 holds).  32 values of which one is not
+ * finite are NaN (scale byte 255, codes 0).  Blocks lie in the order in which the attention's matrix instructions
+ * take them, an even code in the low half of its byte:
+ *   k_pool   [n_blocks, Hkv, 2, 64, 32]   channels 64 a .. 64 a + 63 of token t at [a, t]
+ *   k_scale  [n_blocks, Hkv, 2, 32, 4]    of channels 64 a + 32 g .. + 31 of token t at [g, t % 32, 2 (t / 32) + a]
+ *   v_pool   [n_blocks, Hkv, 128, 32]     of channel c at [c] first the tokens t with t / 4 even, then the others,
+ *                                         each in ascending order
+ *   v_scale  [n_blocks, Hkv, 2, 32, 4]    of channel c and the tokens with t / 4 % 2 = g at [g, c % 32, c / 32]
+ * ------------------------------------------------------------------------------------------- */
+typedef struct {
+  int32_t B, Hkv, D;                /* D must be 128; B <= 4096 */
+  int32_t n_blocks;                 /* 1 .. 2^24 */
+  void* k_pool;                     /* DEVICE, 16-byte aligned */
+  void* v_pool;
+  uint8_t* k_scale;                 /* DEVICE, 4-byte aligned */
+  uint8_t* v_scale;
+  void* k_tail;                     /* DEVICE bf16 [B, Hkv, 128, 128]: the ring, as in 8 bits */
+  void* v_tail;
+} lvspec_paged_mx_cache;
+
+/* New rows of one layer, as lvspec_paged_append; with rot.dim > 0 keys and queries are rotated on the way, as in
+ * lvspec_paged_append_rotary (rot.dim = 0: k as it is, and no queries). */
+typedef struct {
+  lvspec_paged_mx_cache cache;
+  int32_t n_rows;                   /* packed rows, 0 .. 2^28 */
+  const void* k;                    /* DEVICE bf16 [n_rows, Hkv, 128] */
+  const void* v;
+  int64_t k_sr, k_sh, v_sr, v_sh;
+  const int32_t* slots;             /* DEVICE [n_rows], and the other maps of lvspec_paged_plan */
+  const int32_t* row_seq;
+  const int32_t* row_pos;
+  const int32_t* cu_rows;           /* DEVICE [B + 1] */
+  lvspec_rotation rot;
+  int32_t Hq;
+  const void* q;
+  int64_t q_sr, q_sh;
+  void* q_out;
+  int64_t qo_sr, qo_sh;
+} lvspec_paged_mx_append_args;
+
+int lvspec_paged_mx_append(const lvspec_paged_mx_append_args* args, void* stream);
+
+/* Rows out of the cache, in bf16 (exact): row t is the one at slots[t], of the pool or of the ring.  What attention
+ * over a prompt's earlier pieces reads, where its next piece is many rows.  Rows whose slot names no block of the pool
+ * or no row of the ring are left as they are.  A slot may be named any number of times. */
+typedef struct {
+  lvspec_paged_mx_cache cache;
+  int32_t n_rows;                   /* 0 .. 2^28 */
+  const int32_t* slots;             /* DEVICE [n_rows] */
+  void* k;                          /* DEVICE out bf16 [n_rows, Hkv, 128]; must not overlap the cache */
+  void* v;
+  int64_t k_sr, k_sh, v_sr, v_sh;
+} lvspec_paged_mx_read_args;
+
+int lvspec_paged_mx_read(const lvspec_paged_mx_read_args* args, void* stream);
+
+/* Verification attention, as lvspec_verify_attn_paged. */
+typedef struct {
+  lvspec_paged_mx_cache cache;
+  int32_t gamma, Hq;                /* Hq % Hkv == 0; 1 <= gamma <= 32 */
+  const void* q;                    /* DEVICE bf16 [B, gamma, Hq, 128] */
+  int64_t q_sb, q_sg, q_sh;
+  const int32_t* table;             /* DEVICE [B, table_cols]; may be NULL when table_cols == 0 */
+  int32_t table_cols;
+  const int32_t* kv_len;            /* DEVICE [B] */
+  const int32_t* vis_begin;         /* DEVICE [B] or NULL */
+  const int32_t* vis_end;
+  const uint32_t* draft_mask;       /* HOST [gamma] or NULL */
+  float scale;                      /* 0 = 1/sqrt(D) */
+  void* out;                        /* DEVICE bf16 [B, gamma, Hq, 128] */
+  int64_t o_sb, o_sg, o_sh;
+  float* lse;                       /* DEVICE fp32 [B, Hq, gamma] or NULL */
+  float* vis_mass;                  /* DEVICE fp32 [B, Hq, gamma] or NULL (needs vis_begin/end) */
+  void* workspace;                  /* DEVICE */
+  size_t workspace_bytes;
+} lvspec_paged_mx_attn_args;
+
+size_t lvspec_verify_attn_paged_mx_workspace(const lvspec_paged_mx_attn_args* args);
+int lvspec_verify_attn_paged_mx(const lvspec_paged_mx_attn_args* args, void* stream);
+
+/* Committing a verified step, as lvspec_paged_commit. */
+typedef struct {
+  lvspec_paged_mx_cache cache;        /* of the first layer */
+  int32_t n_layers;                 /* 1 .. 65535 */
+  int32_t n_branches, chain_len;
+  const int32_t* table;             /* DEVICE [B, table_cols] */
+  int32_t table_cols;
+  const int32_t* kv_len;            /* DEVICE [B] */
+  const int32_t* accept_len;        /* DEVICE [B * n_branches] */
+  const int32_t* best_branch;       /* DEVICE [B] or NULL */
+  int32_t* new_len;                 /* DEVICE out [B]; must not alias kv_len */
+  const int32_t* granted;           /* DEVICE [B] of the step's plan, or NULL */
+  const int32_t* held;
+  const int32_t* cu_rows;
+} lvspec_paged_mx_commit_args;
+
+int lvspec_paged_mx_commit(const lvspec_paged_mx_commit_args* args, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Diagnostics: how the three verify calls would be launched for the given shapes (no paper
  * passage behind this one: it reports the library's own launch planning, for tuning and tests).
  * Any of the argument pointers may be NULL; its fields of *out are then left untouched.  Only

@@ -28,8 +28,10 @@ STATIC_SCRATCH_BYTES = 16 << 20
 REJECT, EXACT, LOOSE, SHIFT, GATED = 0, 1, 2, 3, 4
 RULE_VISUAL, RULE_ENTROPY_GATE, RULE_ENTROPY_WINDOW = 0, 1, 2
 MAX_GAMMA, MAX_TOPK, MAX_TOPN = 16, 16, 1024
-PAGE_TOKENS, TAIL_ROWS = 64, 128          # of the paged cache in 8 bits
+PAGE_TOKENS, TAIL_ROWS = 64, 128          # of the paged caches
 SLOT_NONE, SLOT_TAIL = -1, -2
+BF16, F16, F32 = 0, 1, 2                  # types of rotary rows
+SCALING_NONE, SCALING_LINEAR, SCALING_NTK, SCALING_YARN = 0, 1, 2, 3
 
 
 class AttnArgs(C.Structure):
@@ -152,6 +154,65 @@ class PagedCommitArgs(C.Structure):
     ]
 
 
+class Rotation(C.Structure):
+    _fields_ = [
+        ("dim", C.c_int32), ("interleaved", C.c_int32), ("transpose", C.c_int32), ("n_axes", C.c_int32),
+        ("inv_freq", C.c_void_p), ("axis", C.c_void_p), ("pos", C.c_void_p), ("pos_sa", C.c_int64),
+        ("factor", C.c_float),
+    ]
+
+
+class RotaryArgs(C.Structure):
+    _fields_ = [
+        ("rot", Rotation),
+        ("n_rows", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32), ("dtype", C.c_int32),
+        ("q", C.c_void_p), ("q_sr", C.c_int64), ("q_sh", C.c_int64),
+        ("q_out", C.c_void_p), ("qo_sr", C.c_int64), ("qo_sh", C.c_int64),
+        ("k", C.c_void_p), ("k_sr", C.c_int64), ("k_sh", C.c_int64),
+        ("k_out", C.c_void_p), ("ko_sr", C.c_int64), ("ko_sh", C.c_int64),
+    ]
+
+
+class RotaryFreqArgs(C.Structure):
+    _fields_ = [("dim", C.c_int32), ("scaling", C.c_int32)] + [
+        (n, C.c_double) for n in ("base", "scale", "original_len", "beta_fast", "beta_slow")]
+
+
+_ROTATED_QUERIES = [
+    ("rot", Rotation), ("Hq", C.c_int32),
+    ("q", C.c_void_p), ("q_sr", C.c_int64), ("q_sh", C.c_int64),
+    ("q_out", C.c_void_p), ("qo_sr", C.c_int64), ("qo_sh", C.c_int64),
+]
+
+
+class PagedAppendRotaryArgs(C.Structure):
+    _fields_ = [("rows", PagedAppendArgs)] + _ROTATED_QUERIES
+
+
+class PagedMxCacheStruct(C.Structure):
+    _fields_ = PagedCacheStruct._fields_
+
+
+class PagedMxAppendArgs(C.Structure):
+    _fields_ = [("cache", PagedMxCacheStruct)] + PagedAppendArgs._fields_[1:] + _ROTATED_QUERIES
+
+
+class PagedMxReadArgs(C.Structure):
+    _fields_ = [
+        ("cache", PagedMxCacheStruct), ("n_rows", C.c_int32), ("slots", C.c_void_p),
+        ("k", C.c_void_p), ("v", C.c_void_p),
+        ("k_sr", C.c_int64), ("k_sh", C.c_int64), ("v_sr", C.c_int64), ("v_sh", C.c_int64),
+    ]
+
+
+class PagedMxAttnArgs(C.Structure):
+    _fields_ = [("cache", PagedMxCacheStruct)] + PagedAttnArgs._fields_[1:]
+
+
+class PagedMxCommitArgs(C.Structure):
+    _fields_ = [("cache", PagedMxCacheStruct)] + PagedCommitArgs._fields_[1:]
+
+
 class PlanInfo(C.Structure):
     _fields_ = [(n, C.c_int32) for n in (
         "attn_rows_padded", "attn_row_chunks", "attn_splits", "rel_splits", "rel_stage_bytes",
@@ -188,12 +249,25 @@ for _name, _t in (("paged_plan", PagedPlanArgs), ("paged_append", PagedAppendArg
 _lib.lvspec_verify_attn_paged_workspace.restype = C.c_size_t
 _lib.lvspec_verify_attn_paged_workspace.argtypes = [C.POINTER(PagedAttnArgs)]
 
+for _name, _t in (("rotary", RotaryArgs), ("paged_append_rotary", PagedAppendRotaryArgs),
+                  ("paged_mx_append", PagedMxAppendArgs), ("paged_mx_read", PagedMxReadArgs),
+                  ("verify_attn_paged_mx", PagedMxAttnArgs), ("paged_mx_commit", PagedMxCommitArgs)):
+    getattr(_lib, f"lvspec_{_name}").restype = C.c_int
+    getattr(_lib, f"lvspec_{_name}").argtypes = [C.POINTER(_t), C.c_void_p]
+_lib.lvspec_verify_attn_paged_mx_workspace.restype = C.c_size_t
+_lib.lvspec_verify_attn_paged_mx_workspace.argtypes = [C.POINTER(PagedMxAttnArgs)]
+_lib.lvspec_rotary_frequencies.restype = C.c_int
+_lib.lvspec_rotary_frequencies.argtypes = [C.POINTER(RotaryFreqArgs), C.POINTER(C.c_float), C.POINTER(C.c_float)]
+
 EXPORTS = ["lvspec_hv_prepare", "lvspec_verify_attn_static", "lvspec_status_string", "lvspec_version", "lvspec_last_hip_error", "lvspec_n_loose",
            "lvspec_verify_attn_workspace", "lvspec_verify_attn",
            "lvspec_visual_relevance_workspace", "lvspec_visual_relevance",
            "lvspec_loose_accept_workspace", "lvspec_loose_accept", "lvspec_kv_commit",
            "lvspec_describe_plan", "lvspec_paged_plan", "lvspec_paged_append",
-           "lvspec_verify_attn_paged_workspace", "lvspec_verify_attn_paged", "lvspec_paged_commit"]
+           "lvspec_verify_attn_paged_workspace", "lvspec_verify_attn_paged", "lvspec_paged_commit",
+           "lvspec_rotary", "lvspec_rotary_frequencies", "lvspec_paged_append_rotary",
+           "lvspec_paged_mx_append", "lvspec_paged_mx_read", "lvspec_verify_attn_paged_mx_workspace",
+           "lvspec_verify_attn_paged_mx", "lvspec_paged_mx_commit"]
 
 
 class LvspecError(RuntimeError):
@@ -657,11 +731,10 @@ def paged_plan(kv_len, n_new, held, queue, state, table, *, max_rows, reserve=0,
     return outs
 
 
-def paged_append_args(cache: PagedCache, k, v, plan) -> PagedAppendArgs:
+def _fill_append(a, cache, k, v, plan):
+    """The packed rows of an append, a.cache set."""
     i32 = torch.int32
-    a = PagedAppendArgs()
     _one_device(*cache, k, v, plan["slots"], plan["row_seq"], plan["row_pos"], plan["cu_rows"])
-    a.cache = _cache_struct(cache)
     n = k.shape[0]
     assert k.is_cuda and v.is_cuda and k.dtype == torch.bfloat16 and v.dtype == torch.bfloat16 and k.shape == v.shape
     assert k.shape[1:] == (a.cache.Hkv, 128) and k.stride(-1) == 1 and v.stride(-1) == 1
@@ -670,6 +743,12 @@ def paged_append_args(cache: PagedCache, k, v, plan) -> PagedAppendArgs:
     a.slots, a.row_seq, a.row_pos = (_dense(plan[x], i32, (n,)) for x in ("slots", "row_seq", "row_pos"))
     a.cu_rows = _dense(plan["cu_rows"], i32, (a.cache.B + 1,))
     return a
+
+
+def paged_append_args(cache: PagedCache, k, v, plan) -> PagedAppendArgs:
+    a = PagedAppendArgs()
+    a.cache = _cache_struct(cache)
+    return _fill_append(a, cache, k, v, plan)
 
 
 def paged_append(cache: PagedCache, k, v, plan, *, stream=None) -> None:
@@ -681,10 +760,15 @@ def paged_append(cache: PagedCache, k, v, plan, *, stream=None) -> None:
 
 def verify_attn_paged_args(q, cache: PagedCache, table, kv_len, *, out, vis_begin=None, vis_end=None,
                            draft_mask=None, scale=0.0, lse=None, vis_mass=None) -> PagedAttnArgs:
-    i32 = torch.int32
     a = PagedAttnArgs()
-    _one_device(*cache, q, table, kv_len, out, vis_begin, vis_end, lse, vis_mass)
     a.cache = _cache_struct(cache)
+    return _fill_attn(a, q, cache, table, kv_len, out, vis_begin, vis_end, draft_mask, scale, lse, vis_mass)
+
+
+def _fill_attn(a, q, cache, table, kv_len, out, vis_begin, vis_end, draft_mask, scale, lse, vis_mass):
+    """The other fields of an attention over a paged cache, a.cache set."""
+    i32 = torch.int32
+    _one_device(*cache, q, table, kv_len, out, vis_begin, vis_end, lse, vis_mass)
     B, gamma, Hq, D = q.shape
     assert q.is_cuda and out.is_cuda and q.dtype == torch.bfloat16 and out.dtype == torch.bfloat16
     assert out.shape == q.shape
@@ -711,16 +795,22 @@ def verify_attn_paged(q, cache: PagedCache, table, kv_len, *, vis_begin=None, vi
                       stream=None):
     """lvspec_verify_attn_paged.  q bf16 [B,gamma,Hq,128], one layer's cache, table int32 [B,cols], kv_len
     int32 [B].  Returns out, or (out, lse, vis_mass) when either extra is asked for."""
+    return _attn(verify_attn_paged_args, "verify_attn_paged", q, cache, table, kv_len, vis_begin, vis_end, draft_mask,
+                 scale, out, return_lse, return_vis_mass, workspace, stream)
+
+
+def _attn(make, name, q, cache, table, kv_len, vis_begin, vis_end, draft_mask, scale, out, return_lse, return_vis_mass,
+          workspace, stream):
     B, gamma, Hq, _ = q.shape
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     lse = q.new_empty((B, Hq, gamma), dtype=torch.float32) if return_lse else None
     vm = q.new_empty((B, Hq, gamma), dtype=torch.float32) if return_vis_mass else None
-    a = verify_attn_paged_args(q, cache, table, kv_len, out=out, vis_begin=vis_begin, vis_end=vis_end,
-                               draft_mask=draft_mask, scale=scale, lse=lse, vis_mass=vm)
-    ws = _workspace(_lib.lvspec_verify_attn_paged_workspace(C.byref(a)), q, workspace)
+    a = make(q, cache, table, kv_len, out=out, vis_begin=vis_begin, vis_end=vis_end, draft_mask=draft_mask, scale=scale,
+             lse=lse, vis_mass=vm)
+    ws = _workspace(getattr(_lib, f"lvspec_{name}_workspace")(C.byref(a)), q, workspace)
     a.workspace, a.workspace_bytes = ws.data_ptr(), ws.numel() * ws.element_size()
-    _call_on(q.device, _lib.lvspec_verify_attn_paged, a, stream)
+    _call_on(q.device, getattr(_lib, f"lvspec_{name}"), a, stream)
     if return_lse or return_vis_mass:
         return out, lse, vm
     return out
@@ -728,12 +818,17 @@ def verify_attn_paged(q, cache: PagedCache, table, kv_len, *, vis_begin=None, vi
 
 def paged_commit_args(cache: PagedCache, table, kv_len, accept_len, chain_len, *, best_branch=None, n_branches=1,
                       new_len, plan=None) -> PagedCommitArgs:
-    i32 = torch.int32
-    layers = cache.k_pool.shape[0] if cache.k_pool.dim() == 5 else 1
     a = PagedCommitArgs()
+    layers = cache.k_pool.shape[0] if cache.k_pool.dim() == 5 else 1
+    a.cache = _cache_struct(cache, (layers,) if cache.k_pool.dim() == 5 else ())
+    return _fill_commit(a, layers, cache, table, kv_len, accept_len, chain_len, best_branch, n_branches, new_len, plan)
+
+
+def _fill_commit(a, layers, cache, table, kv_len, accept_len, chain_len, best_branch, n_branches, new_len, plan):
+    """The other fields of a commit to a paged cache, a.cache set."""
+    i32 = torch.int32
     given = () if plan is None else (plan["granted"], plan["new_held"], plan["cu_rows"])
     _one_device(*cache, table, kv_len, accept_len, best_branch, new_len, *given)
-    a.cache = _cache_struct(cache, (layers,) if cache.k_pool.dim() == 5 else ())
     B = a.cache.B
     a.n_layers, a.n_branches, a.chain_len = layers, int(n_branches), int(chain_len)
     a.table, a.table_cols = _dense(table, i32, (B, table.shape[1])), table.shape[1]
@@ -757,4 +852,231 @@ def paged_commit(cache: PagedCache, table, kv_len, accept_len, chain_len, *, bes
     a = paged_commit_args(cache, table, kv_len, accept_len, chain_len, best_branch=best_branch,
                           n_branches=n_branches, new_len=new_len, plan=plan)
     _call_on(table.device, _lib.lvspec_paged_commit, a, stream)
+    return new_len
+
+
+# ------------------------------------------------------------------ rotary positions
+class Rotary(NamedTuple):
+    """How rows are turned: frequencies and factor as rotary_frequencies gives them."""
+    inv_freq: torch.Tensor                  # fp32 [dim / 2] on the device
+    factor: float = 1.0
+    interleaved: bool = False
+    axis: Optional[torch.Tensor] = None     # uint8 [dim / 2]: which of a token's positions a frequency goes by
+
+
+def rotary_frequencies(dim, base=10000.0, *, scaling=SCALING_NONE, scale=1.0, original_len=0, beta_fast=0.0, beta_slow=0.0,
+                       device=None):
+    """lvspec_rotary_frequencies: (inv_freq fp32 [dim / 2] on `device`, factor)."""
+    a = RotaryFreqArgs(int(dim), int(scaling), float(base), float(scale), float(original_len), float(beta_fast),
+                       float(beta_slow))
+    out, factor = (C.c_float * max(1, int(dim) // 2))(), C.c_float()
+    _check(_lib.lvspec_rotary_frequencies(C.byref(a), out, C.byref(factor)))
+    return torch.tensor(list(out), dtype=torch.float32, device=device), float(factor.value)
+
+
+_ROTARY_TYPES = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}
+
+
+def _fill_rotation(r: Rotation, rot: Rotary, pos, n_rows, transpose=False):
+    inv = rot.inv_freq
+    half = inv.numel()
+    r.dim, r.interleaved, r.transpose = 2 * half, 1 if rot.interleaved else 0, 1 if transpose else 0
+    r.inv_freq = _dense(inv, torch.float32, (half,))
+    r.axis = None if rot.axis is None else _dense(rot.axis, torch.uint8, (half,))
+    r.factor = float(rot.factor)
+    r.n_axes = 1
+    if pos is not None:
+        n_axes = 1 if pos.dim() == 1 else pos.shape[0]
+        assert pos.is_cuda and pos.dtype == torch.int32 and pos.shape[-1] == n_rows and pos.dim() <= 2
+        assert pos.stride(-1) == 1 or n_rows <= 1
+        r.n_axes, r.pos, r.pos_sa = n_axes, pos.data_ptr(), pos.stride(0) if pos.dim() == 2 and n_axes > 1 else 0
+    assert rot.axis is not None or r.n_axes == 1
+
+
+def _rows_of(x, dtype, n_rows):
+    """[n_rows, H, D] with rows of contiguous channels: (data, row and head strides, in 16 bytes where there is one)."""
+    n, H, D = x.shape
+    assert x.is_cuda and x.dtype == dtype and n == n_rows and (x.stride(-1) == 1 or D == 1)
+    most = -(-D // 8) * 8
+    return x.data_ptr(), x.stride(0) if n > 1 else max(most, H * most), x.stride(1) if H > 1 else most
+
+
+def _fill_queries(a, q, q_out, n_rows):
+    a.Hq = 0
+    if q is not None:
+        assert q_out is not None and q_out.shape == q.shape
+        a.Hq = q.shape[1]
+        a.q, a.q_sr, a.q_sh = _rows_of(q, torch.bfloat16, n_rows)
+        a.q_out, a.qo_sr, a.qo_sh = _rows_of(q_out, torch.bfloat16, n_rows)
+
+
+def rotary_args(q, pos, rot: Rotary, *, out, k=None, k_out=None, transpose=False) -> RotaryArgs:
+    a = RotaryArgs()
+    _one_device(q, pos, out, k, k_out, rot.inv_freq, rot.axis)
+    n, Hq, D = q.shape
+    _fill_rotation(a.rot, rot, pos, n, transpose)
+    a.n_rows, a.Hq, a.Hkv, a.D, a.dtype = n, Hq, 0, D, _ROTARY_TYPES[q.dtype]
+    assert out.shape == q.shape
+    a.q, a.q_sr, a.q_sh = _rows_of(q, q.dtype, n)
+    a.q_out, a.qo_sr, a.qo_sh = _rows_of(out, q.dtype, n)
+    if k is not None:
+        assert k.shape[2] == D and k_out is not None and k_out.shape == k.shape
+        a.Hkv = k.shape[1]
+        a.k, a.k_sr, a.k_sh = _rows_of(k, q.dtype, n)
+        a.k_out, a.ko_sr, a.ko_sh = _rows_of(k_out, q.dtype, n)
+    return a
+
+
+@_allocates_on_stream
+def rotary(q, pos, rot: Rotary, *, k=None, out=None, k_out=None, transpose=False, stream=None):
+    """lvspec_rotary.  q [n_rows,Hq,D] and k [n_rows,Hkv,D] (optional) bf16, fp16 or fp32; pos int32 [n_rows], or
+    [n_axes,n_rows] with rot.axis.  out and k_out may be q and k.  transpose: turned back, the gradient of q (and k)
+    from that of out.  Returns out, or (out, k_out)."""
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    if k is not None and k_out is None:
+        k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
+    a = rotary_args(q, pos, rot, out=out, k=k, k_out=k_out, transpose=transpose)
+    _call_on(q.device, _lib.lvspec_rotary, a, stream)
+    return out if k is None else (out, k_out)
+
+
+def paged_append_rotary_args(cache: PagedCache, k, v, plan, rot: Rotary, *, pos=None, q=None, q_out=None) -> PagedAppendRotaryArgs:
+    a = PagedAppendRotaryArgs()
+    _one_device(k, pos, q, q_out, rot.inv_freq, rot.axis)
+    a.rows = paged_append_args(cache, k, v, plan)
+    _fill_rotation(a.rot, rot, pos, k.shape[0])
+    _fill_queries(a, q, q_out, k.shape[0])
+    return a
+
+
+@_allocates_on_stream
+def paged_append_rotary(cache: PagedCache, k, v, plan, rot: Rotary, *, pos=None, q=None, q_out=None, stream=None):
+    """lvspec_paged_append_rotary: paged_append of k as rot turns it.  pos int32 [n_rows] or [n_axes,n_rows] (None: the
+    rows' places in the cache); q bf16 [n_rows,Hq,128] is turned in the same launch.  Returns q_out (None without q).
+    A q_out that is allocated here holds zeros where there is no row."""
+    if q is not None and q_out is None:
+        q_out = torch.zeros_like(q, memory_format=torch.contiguous_format)
+    a = paged_append_rotary_args(cache, k, v, plan, rot, pos=pos, q=q, q_out=q_out)
+    _call_on(k.device, _lib.lvspec_paged_append_rotary, a, stream)
+    return q_out
+
+
+# ------------------------------------------------------------------ paged cache in 4 bits
+class PagedMxCache(NamedTuple):
+    """The arrays of one layer, or of several with a leading dimension (include/lvspec.h says what
+    they hold).  Plans, tables and slots are those of the cache in 8 bits."""
+    k_pool: torch.Tensor      # uint8 [n_blocks, Hkv, 2, 64, 32]
+    v_pool: torch.Tensor      # uint8 [n_blocks, Hkv, 128, 32]
+    k_scale: torch.Tensor     # uint8 [n_blocks, Hkv, 2, 32, 4]
+    v_scale: torch.Tensor
+    k_tail: torch.Tensor      # bf16 [B, Hkv, 128, 128]
+    v_tail: torch.Tensor
+
+    def layer(self, i: int) -> "PagedMxCache":
+        return PagedMxCache(*[x[i] for x in self])
+
+
+def _paged_mx_shapes(B, Hkv, n_blocks):
+    pool = (n_blocks, Hkv)
+    return [((*pool, 2, PAGE_TOKENS, 32), torch.uint8), ((*pool, 128, 32), torch.uint8),
+            ((*pool, 2, 32, 4), torch.uint8), ((*pool, 2, 32, 4), torch.uint8),
+            ((B, Hkv, TAIL_ROWS, 128), torch.bfloat16), ((B, Hkv, TAIL_ROWS, 128), torch.bfloat16)]
+
+
+def alloc_paged_mx_cache(B, Hkv, n_blocks, device, layers: Optional[int] = None) -> PagedMxCache:
+    lead = () if layers is None else (layers,)
+    return PagedMxCache(*[torch.zeros(lead + s, dtype=t, device=device) for s, t in _paged_mx_shapes(B, Hkv, n_blocks)])
+
+
+def _cache4_struct(cache: PagedMxCache, lead=()) -> PagedMxCacheStruct:
+    n_blocks, Hkv = cache.k_pool.shape[len(lead):len(lead) + 2]
+    s = PagedMxCacheStruct()
+    s.B, s.Hkv, s.D, s.n_blocks = cache.k_tail.shape[len(lead)], Hkv, 128, n_blocks
+    for name, x, (shape, dtype) in zip(PagedMxCache._fields, cache, _paged_mx_shapes(s.B, Hkv, n_blocks)):
+        setattr(s, name, _dense(x, dtype, (*lead, *shape)))
+    return s
+
+
+def paged_mx_append_args(cache: PagedMxCache, k, v, plan, *, rot: Optional[Rotary] = None, pos=None, q=None,
+                       q_out=None) -> PagedMxAppendArgs:
+    a = PagedMxAppendArgs()
+    a.cache = _cache4_struct(cache)
+    _fill_append(a, cache, k, v, plan)
+    if rot is None:
+        assert pos is None and q is None
+        return a
+    _one_device(k, pos, q, q_out, rot.inv_freq, rot.axis)
+    _fill_rotation(a.rot, rot, pos, k.shape[0])
+    _fill_queries(a, q, q_out, k.shape[0])
+    return a
+
+
+@_allocates_on_stream
+def paged_mx_append(cache: PagedMxCache, k, v, plan, *, rot: Optional[Rotary] = None, pos=None, q=None, q_out=None,
+                  stream=None):
+    """lvspec_paged_mx_append: as paged_append or, with rot, as paged_append_rotary."""
+    if q is not None and q_out is None:
+        q_out = torch.zeros_like(q, memory_format=torch.contiguous_format)
+    a = paged_mx_append_args(cache, k, v, plan, rot=rot, pos=pos, q=q, q_out=q_out)
+    _call_on(k.device, _lib.lvspec_paged_mx_append, a, stream)
+    return q_out
+
+
+def paged_mx_read_args(cache: PagedMxCache, slots, *, k, v) -> PagedMxReadArgs:
+    a = PagedMxReadArgs()
+    _one_device(*cache, slots, k, v)
+    a.cache = _cache4_struct(cache)
+    n = slots.shape[0]
+    a.n_rows, a.slots = n, _dense(slots, torch.int32, (n,))
+    assert k.shape == v.shape == (n, a.cache.Hkv, 128)
+    a.k, a.k_sr, a.k_sh = _rows_of(k, torch.bfloat16, n)
+    a.v, a.v_sr, a.v_sh = _rows_of(v, torch.bfloat16, n)
+    return a
+
+
+@_allocates_on_stream
+def paged_mx_read(cache: PagedMxCache, slots, *, k=None, v=None, stream=None):
+    """lvspec_paged_mx_read: the rows at slots int32 [n_rows] (a plan's, say), bf16 [n_rows,Hkv,128].  Returns (k, v);
+    what is allocated here holds zeros where a slot names no row."""
+    shape = (slots.shape[0], cache.k_tail.shape[1], 128)
+    k, v = (torch.zeros(shape, dtype=torch.bfloat16, device=slots.device) if x is None else x for x in (k, v))
+    a = paged_mx_read_args(cache, slots, k=k, v=v)
+    _call_on(slots.device, _lib.lvspec_paged_mx_read, a, stream)
+    return k, v
+
+
+def verify_attn_paged_mx_args(q, cache: PagedMxCache, table, kv_len, *, out, vis_begin=None, vis_end=None,
+                            draft_mask=None, scale=0.0, lse=None, vis_mass=None) -> PagedMxAttnArgs:
+    a = PagedMxAttnArgs()
+    a.cache = _cache4_struct(cache)
+    return _fill_attn(a, q, cache, table, kv_len, out, vis_begin, vis_end, draft_mask, scale, lse, vis_mass)
+
+
+@_allocates_on_stream
+def verify_attn_paged_mx(q, cache: PagedMxCache, table, kv_len, *, vis_begin=None, vis_end=None, draft_mask=None,
+                       scale=0.0, out=None, return_lse=False, return_vis_mass=False, workspace=None,
+                       stream=None):
+    """lvspec_verify_attn_paged_mx: as verify_attn_paged."""
+    return _attn(verify_attn_paged_mx_args, "verify_attn_paged_mx", q, cache, table, kv_len, vis_begin, vis_end, draft_mask,
+                 scale, out, return_lse, return_vis_mass, workspace, stream)
+
+
+def paged_mx_commit_args(cache: PagedMxCache, table, kv_len, accept_len, chain_len, *, best_branch=None, n_branches=1,
+                       new_len, plan=None) -> PagedMxCommitArgs:
+    a = PagedMxCommitArgs()
+    layers = cache.k_pool.shape[0] if cache.k_pool.dim() == 6 else 1
+    a.cache = _cache4_struct(cache, (layers,) if cache.k_pool.dim() == 6 else ())
+    return _fill_commit(a, layers, cache, table, kv_len, accept_len, chain_len, best_branch, n_branches, new_len, plan)
+
+
+@_allocates_on_stream
+def paged_mx_commit(cache: PagedMxCache, table, kv_len, accept_len, chain_len, *, best_branch=None, n_branches=1,
+                  new_len=None, plan=None, stream=None):
+    """lvspec_paged_mx_commit: as paged_commit."""
+    if new_len is None:
+        new_len = torch.empty_like(kv_len)
+    a = paged_mx_commit_args(cache, table, kv_len, accept_len, chain_len, best_branch=best_branch,
+                           n_branches=n_branches, new_len=new_len, plan=plan)
+    _call_on(table.device, _lib.lvspec_paged_mx_commit, a, stream)
     return new_len

@@ -250,19 +250,69 @@ struct AppendKernelArgs {
   const int32_t* cu_rows;
   uint8_t* k8;
   uint8_t* v8;
-  float* k_scale;
-  float* v_scale;
+  void* k_scale;                // float, in the cache of 4 bits exponents
+  void* v_scale;
   uint8_t* k_tail;
   uint8_t* v_tail;
   int n_rows, B, Hkv, n_blocks;
 };
 hipError_t launch_paged_append(const AppendKernelArgs& a, hipStream_t stream);
 
+hipError_t launch_paged_mx_append(const AppendKernelArgs& a, hipStream_t stream);
+
+// ---------------------------------------------------------------- rotary positions
+struct RotaryKernelArgs {
+  const float* inv_freq;        // [half]
+  const uint8_t* axis;          // [half] or nullptr: the first
+  const int32_t* pos;           // [n_axes] at pos_sa, [n_rows]
+  int64_t pos_sa;
+  int half, interleaved, n_axes;
+  double factor, sine;          // of the cosines, and of the sines (negative: turned back)
+};
+struct RotaryRows {             // strides in elements
+  const void* x;
+  void* y;
+  int64_t x_sr, x_sh, y_sr, y_sh;
+  int H;                        // 0: none
+};
+struct RotaryCallArgs {
+  RotaryKernelArgs rot;
+  RotaryRows q, k;
+  int64_t n_rows;
+  int D, in_place;
+  int pieces, heads;            // pieces of a row, heads of a thread (of the launch)
+};
+constexpr int kRotaryEnough = 1 << 17;      // threads that fill the chip
+hipError_t launch_rotary(const RotaryCallArgs& a, int dtype, hipStream_t stream);
+
+struct AppendRotaryKernelArgs {
+  AppendKernelArgs rows;
+  RotaryKernelArgs rot;
+  RotaryRows q;
+  int k_heads, k_groups, q_heads, q_wgs;    // (of the launch)
+};
+hipError_t launch_paged_append_rotary(const AppendRotaryKernelArgs& a, bool four, hipStream_t stream);
+
+struct ReadKernelArgs {
+  const uint8_t* k4;
+  const uint8_t* v4;
+  const uint8_t* k_scale;
+  const uint8_t* v_scale;
+  const uint8_t* k_tail;
+  const uint8_t* v_tail;
+  const int32_t* slots;
+  uint8_t* k;
+  uint8_t* v;
+  int64_t k_sr, k_sh, v_sr, v_sh;      // bytes
+  int n_rows, B, Hkv, n_blocks;
+};
+hipError_t launch_paged_mx_read(const ReadKernelArgs& a, hipStream_t stream);
+
 struct PagedCommitKernelArgs {
   uint8_t* k8;
   uint8_t* v8;
-  float* k_scale;
-  float* v_scale;
+  void* k_scale;                // float, in the cache of 4 bits exponents
+  void* v_scale;
   uint8_t* k_tail;
   uint8_t* v_tail;
   const int32_t* table;
@@ -276,14 +326,15 @@ struct PagedCommitKernelArgs {
   int B, Hkv, n_layers, n_branches, chain_len, n_blocks, cols;
 };
 hipError_t launch_paged_commit(const PagedCommitKernelArgs& a, hipStream_t stream);
+hipError_t launch_paged_mx_commit(const PagedCommitKernelArgs& a, hipStream_t stream);
 
 struct PagedAttnKernelArgs {
   const uint16_t* q;
   int64_t q_sb, q_sg, q_sh;
   const uint8_t* k8;
   const uint8_t* v8;
-  const float* k_scale;
-  const float* v_scale;
+  const void* k_scale;          // float, in the cache of 4 bits exponents
+  const void* v_scale;
   const uint8_t* k_tail;
   const uint8_t* v_tail;
   const int32_t* table;
@@ -305,5 +356,7 @@ struct PagedAttnKernelArgs {
   uint32_t draft_mask[32];
 };
 hipError_t launch_paged_attn(const PagedAttnKernelArgs& a, hipStream_t stream);
+hipError_t launch_paged_mx_attn(const PagedAttnKernelArgs& a, hipStream_t stream);
+hipError_t launch_paged_combine(const PagedAttnKernelArgs& a, hipStream_t stream);      // second kernel of both
 
 }  // namespace lvspec

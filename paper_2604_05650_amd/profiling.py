@@ -130,6 +130,12 @@ GROUPS = {   # kernels launched by one call of each entry point
     "paged_append": ("paged_append_kernel",),
     "verify_attn_paged": ("paged_attn_kernel", "paged_attn_unit_kernel", "paged_combine_kernel"),
     "paged_commit": ("paged_commit_kernel",),
+    "rotary": ("rotary_kernel",),
+    "paged_append_rotary": ("paged_append_rotary_kernel",),       # (paged_mx_append too, with a rotation)
+    "paged_mx_append": ("paged_mx_append_kernel",),
+    "paged_mx_read": ("paged_mx_read_kernel",),
+    "verify_attn_paged_mx": ("paged_mx_attn_kernel", "paged_mx_attn_unit_kernel", "paged_combine_kernel"),
+    "paged_mx_commit": ("paged_mx_commit_kernel",),
 }
 # of these, the kernels that stream, by the start of their names
 STREAMS = {
