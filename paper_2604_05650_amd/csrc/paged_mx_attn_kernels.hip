@@ -2,15 +2,70 @@
 // the cache in 8 bits (paged_segment.h).
 //
 // A wave takes every KS-th tile of 64 keys of its workgroup's part.  A tile's codes lie in memory as the lanes take
-// them: they are loaded straight into registers, 1 KiB in one piece per instruction, and widened to bf16 with their
-// scales (exact).  S^T = K Q^T leaves a row's scores in the lanes that hold the values of their tokens, so
-// probabilities (rounded to bf16, each by at most 2^-8 of itself) go into the second product where they are.
+// them: they are loaded straight into registers, 1 KiB in one piece per instruction.
+//   S^T = K Q^T: keys go into the matrix instructions as they are, with their scales.  What they meet are sums of three
+//     numbers of 6 bits (e2m3, 1 to 7.5 in steps of an eighth to a half, and down to an eighth) with a power of two per
+//     row and 32 channels: of a bf16 number within 2^-7 of the largest of its 32 nothing is lost, of a smaller one at
+//     most 2^-15 of that largest.  12 instructions of half the time instead of 16 of bf16, and no keys to widen.
+//   O^T = V^T P^T: scores are left in the lanes that hold the values of their tokens, so probabilities, rounded to bf16
+//     (each by at most 2^-8 of itself), go into the second product where they are; values are widened to bf16 with
+//     their scales (exact).  In numbers of 6 bits probabilities take three as well, whose making costs what the
+//     widening does, and what is far below the largest of its 32 loses its last bits.
 #include "paged_mx_dev.h"
 #include "paged_segment.h"
 
 namespace lvspec {
 
 namespace {
+
+// 32 numbers of 6 bits.
+typedef uint32_t Six __attribute__((ext_vector_type(6)));
+typedef float f32x32 __attribute__((ext_vector_type(32)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// x[0] y[0] x[1] y[1] .. / scale to the nearest numbers of 6 bits, and back.  (In assembly: the instructions write their
+// result before they have read all they take, which this compiler does not know; the waits are those between
+// instructions of this kind and what the compiler puts around them.)
+LVS_DEV Six to_six(const f32x16& x, const f32x16& y, float scale) {
+  Six r;
+  asm("s_nop 1\n\tv_cvt_scalef32_2xpk16_fp6_f32 %0, %1, %2, %3\n\ts_nop 1" : "=&v"(r) : "v"(x), "v"(y), "v"(scale));
+  return r;
+}
+LVS_DEV f32x32 from_six(const Six& x, float scale) {
+  f32x32 r;
+  asm("s_nop 1\n\tv_cvt_scalef32_pk32_f32_fp6 %0, %1, %2\n\ts_nop 1" : "=&v"(r) : "v"(x), "v"(scale));
+  return r;
+}
+
+// Sums of numbers of 6 bits at 2^e, 2^(e - 4), 2^(e - 9): what a term leaves, at most a quarter of its scale, is at most 4
+// of the second's, and what that leaves, an eighth, at most 4 of the third's.
+constexpr int kNext = 4;
+template <int N, class Put>
+LVS_DEV void split6(f32x16 x, f32x16 y, int e, Put&& put) {
+#pragma unroll
+  for (int term = 0; term < N; ++term) {
+    const int at = e - kNext * term - (term == 2 ? 1 : 0);
+    const float scale = __builtin_bit_cast(float, (uint32_t)(at + 127) << 23);
+    const Six v = to_six(x, y, scale);
+    put(term, v);
+    if (term + 1 < N) {
+      const f32x32 z = from_six(v, scale);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        x[i] -= z[2 * i];
+        y[i] -= z[2 * i + 1];
+      }
+    }
+  }
+}
+
+// D += A B, 32x32, 64 deep: A 32 codes of e2m1 a lane, scale in byte KS of ks; B 32 numbers of 6 bits, byte QS of qs.
+template <int KS, int QS>
+LVS_DEV f32x16 mfma_mx(const u32x4& a, uint32_t ks, const Six& b, uint32_t qs, const f32x16& c) {
+  const i32x8 x = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
+  const i32x8 y = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], (int)b[4], (int)b[5], 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 2, KS, (int)ks, QS, (int)qs);
+}
 
 // 32 query rows on 32x32 tiles: the tokens of a lane's scores are those of its values, element 16 t + r is token
 // 32 t + 8 (r / 4) + 4 h + r % 4.
@@ -27,18 +82,52 @@ struct FourRows : WideRows {
     for (int x = 0; x < 8; ++x)
       k[x] = *reinterpret_cast<const u32x4*>(kt + ((p0 + (lane & 31)) & (kTailRows - 1)) * kRowBytes + 2 * channel(x, lane));
   }
-  LVS_DEV void scores4(float (&s)[32], const u32x4 (&k)[4], uint32_t scales) const {
-    const float f[4] = {scale4<0>(scales), scale4<1>(scales), scale4<2>(scales), scale4<3>(scales)};
+  Six q6[3][2];            // term, channels 64 a + 32 h .. + 31
+  uint32_t qs[2];          // their scales' exponents, byte by term
+
+  // From q.  A row's 32 channels of which one is not finite are NaN.
+  LVS_DEV void split_q() {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int a = 0; a < 2; ++a) {
+      uint32_t m = 0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const uint32_t w = q[4 * a + (i >> 2)][i & 3];
+        m = max(m, max(w & 0x7fffu, (w >> 16) & 0x7fffu));
+      }
+      const bool nan = m >= 0x7f80u;
+      const int e = max((int)(m >> 7) - 127 - 2 + ((m & 0x7fu) > 0x70u ? 1 : 0), -100);      // max |q| <= 7.5 * 2^e
+      f32x16 x, y;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const uint32_t w = nan ? 0u : q[4 * a + (i >> 2)][i & 3];
+        x[i] = __builtin_bit_cast(float, w << 16);
+        y[i] = __builtin_bit_cast(float, w & 0xffff0000u);
+      }
+      const uint32_t byte = (uint32_t)(e + 127);
+      qs[a] = nan ? 0xffffffffu : byte | ((byte - kNext) << 8) | ((byte - 2 * kNext - 1) << 16);
+      split6<3>(x, y, e, [&](int term, const Six& v) { q6[term][a] = v; });
+    }
+  }
+
+  LVS_DEV void scores4(float (&s)[32], const u32x4 (&k)[4], uint32_t scales) const {
+    auto tile = [&](auto t) {
       f32x16 z;
 #pragma unroll
       for (int r = 0; r < 16; ++r) z[r] = 0.f;
+      auto half = [&](auto a) {
+        constexpr int ks = 2 * t.value + a.value;
+        z = mfma_mx<ks, 0>(k[2 * a.value + t.value], scales, q6[0][a.value], qs[a.value], z);
+        z = mfma_mx<ks, 1>(k[2 * a.value + t.value], scales, q6[1][a.value], qs[a.value], z);
+        z = mfma_mx<ks, 2>(k[2 * a.value + t.value], scales, q6[2][a.value], qs[a.value], z);
+      };
+      half(std::integral_constant<int, 0>{});
+      half(std::integral_constant<int, 1>{});
 #pragma unroll
-      for (int x = 0; x < 8; ++x) z = mfma32(widen4(k[2 * (x >> 2) + t][x & 3], f[2 * t + (x >> 2)]), q[x], z);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[16 * t + r] = z[r];
-    }
+      for (int r = 0; r < 16; ++r) s[16 * t.value + r] = z[r];
+    };
+    tile(std::integral_constant<int, 0>{});
+    tile(std::integral_constant<int, 1>{});
   }
   LVS_DEV void output4(const u32x4 (&pr)[4], const u32x4 (&v)[4], uint32_t scales) {
     const float f[4] = {scale4<0>(scales), scale4<1>(scales), scale4<2>(scales), scale4<3>(scales)};
@@ -47,13 +136,6 @@ struct FourRows : WideRows {
 #pragma unroll
       for (int c = 0; c < 4; ++c) acc[c] = mfma32(widen4(v[c][y], f[c]), pr[y], acc[c]);
   }
-};
-
-// A tile in registers.
-struct Tile {
-  u32x4 k[4], v[4];
-  uint32_t ks, vs;
-  int id;
 };
 
 template <bool ONCE, class T>
@@ -71,31 +153,12 @@ struct Segment4 : Segment<FourRows, KS, ONCE> {
   using Base::stream;
   LVS_DEV Segment4(const PagedAttnKernelArgs& a, uint8_t* lds) : Base(a, lds) {}
 
-  LVS_DEV void load(Tile& x, int id, int h, int lane) const {
-    x.id = id;
-    const int64_t at = (int64_t)max(id, 0) * p.Hkv + h;
-    const uint8_t* k = p.k8 + at * kPage4Bytes;
-    const uint8_t* v = p.v8 + at * kPage4Bytes;
-    const int off = (lane & 31) * 32 + (lane >> 5) * 16;
-    x.ks = load_once<ONCE, uint32_t>(static_cast<const uint8_t*>(p.k_scale) + at * kScale4Bytes + lane * 4);
+  // a lane's codes and scales of a tile's keys or values
+  LVS_DEV void load(u32x4 (&x)[4], uint32_t& scales, const uint8_t* pool, const void* scale, int64_t at, int lane) const {
+    const uint8_t* from = pool + at * kPage4Bytes + (lane & 31) * 32 + (lane >> 5) * 16;
+    scales = load_once<ONCE, uint32_t>(static_cast<const uint8_t*>(scale) + at * kScale4Bytes + lane * 4);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x.k[i] = load_once<ONCE, u32x4>(k + i * 1024 + off);
-    x.vs = load_once<ONCE, uint32_t>(static_cast<const uint8_t*>(p.v_scale) + at * kScale4Bytes + lane * 4);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x.v[i] = load_once<ONCE, u32x4>(v + i * 1024 + off);
-  }
-
-  LVS_DEV void take(const Tile& x, int tile, int lane) {
-    if (x.id < 0) return;                // (an entry that names no block of the pool: no key)
-    float s[32];
-    st.scores4(s, x.k, x.ks);
-    this->softmax(s, tile * kPageTokens, kPageTokens, [&](int e) { return FourRows::key_of(lane, e); });
-    u32x4 pr[4];
-#pragma unroll
-    for (int y = 0; y < 4; ++y)
-      pr[y] = pack8(s[8 * y], s[8 * y + 1], s[8 * y + 2], s[8 * y + 3], s[8 * y + 4], s[8 * y + 5], s[8 * y + 6],
-                    s[8 * y + 7]);
-    st.output4(pr, x.v, x.vs);
+    for (int i = 0; i < 4; ++i) x[i] = load_once<ONCE, u32x4>(from + i * 1024);
   }
 
   // tiles t0 .. t1-1 of a unit
@@ -104,24 +167,39 @@ struct Segment4 : Segment<FourRows, KS, ONCE> {
     if (mine <= 0) return;
     const int lane = Base::lane_now();
     const int32_t* row = p.table + (int64_t)b * p.cols;
-    int ids;                             // blocks of 64 tiles, one per lane; -1: no block of the pool
+    int ids, id;                         // blocks of 64 tiles, one per lane; -1: no block of the pool
     auto fetch = [&](int j0) {
       const int t = t0 + stream + KS * (j0 + lane);
       ids = t < t1 ? row[t] : -1;
       ids = (uint32_t)ids < (uint32_t)p.n_blocks ? ids : -1;
     };
-    auto next = [&](Tile& x, int j) {
-      if (j >= mine) return;
+    auto place = [&](int j) {            // of the block in the pools; where there is none, of the first
       if ((j & 63) == 0) fetch(j);
-      load(x, __builtin_amdgcn_readlane(ids, j & 63), h, lane);
+      id = __builtin_amdgcn_readlane(ids, j & 63);
+      return (int64_t)max(id, 0) * p.Hkv + h;
     };
-    Tile x, y;
-    next(x, 0);
-    for (int j = 0; j < mine; j += 2) {
-      next(y, j + 1);
-      take(x, t0 + stream + KS * j, lane);
-      next(x, j + 2);
-      if (j + 1 < mine) take(y, t0 + stream + KS * (j + 1), lane);
+    st.split_q();
+    u32x4 k[4], v[4];
+    uint32_t ks, vs;
+    int64_t at = place(0);
+    load(k, ks, p.k8, p.k_scale, at, lane);
+    for (int j = 0; j < mine; ++j) {
+      const bool there = id >= 0;        // (an entry that names no block of the pool: no key)
+      load(v, vs, p.v8, p.v_scale, at, lane);
+      float s[32];
+      st.scores4(s, k, ks);
+      if (j + 1 < mine) {
+        at = place(j + 1);
+        load(k, ks, p.k8, p.k_scale, at, lane);
+      }
+      if (!there) continue;
+      this->softmax(s, (t0 + stream + KS * j) * kPageTokens, kPageTokens, [&](int e) { return FourRows::key_of(lane, e); });
+      u32x4 pr[4];
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+        pr[y] = pack8(s[8 * y], s[8 * y + 1], s[8 * y + 2], s[8 * y + 3], s[8 * y + 4], s[8 * y + 5], s[8 * y + 6],
+                      s[8 * y + 7]);
+      st.output4(pr, v, vs);
     }
   }
 };
@@ -155,8 +233,8 @@ __global__ __launch_bounds__(64 * KS, 2) void paged_mx_attn_unit_kernel(PagedAtt
   const int b = (int)((uint32_t)bh / (uint32_t)p.Hkv), h = bh - b * p.Hkv;
   const int L = paged_len(p.kv_len[b], p.cols);
   sg.begin(b, h, rc);
-  sg.blocks4(b, h, 0, L >> kPageShift);
   sg.open_rows(b, h, rc, L);
+  sg.blocks4(b, h, 0, L >> kPageShift);
   sg.finish(sg.active(L >> kPageShift, true, L), b, h, rc);
 }
 

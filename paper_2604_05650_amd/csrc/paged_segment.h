@@ -177,8 +177,9 @@ LVS_DEV bool finite(float x) { return fabsf(x) <= 3.4028234663852886e38f; }
 // `first`: there is nothing to rescale yet.  The maximum is exact: a reference that is taken anew only for
 // scores 2^8 above it saves 1 to 4 % of the time and costs the exact 1 of the largest probability (error
 // against 64 bits 2.2e-3 -> 2.5e-3).
+// Returned: the lane's largest score, in base 2.
 template <int LANES, int N, class Rescale>
-LVS_DEV void softmax_row(float (&s)[N], float& m, float& l, float c, bool first, Rescale&& rescale) {
+LVS_DEV float softmax_row(float (&s)[N], float& m, float& l, float c, bool first, Rescale&& rescale) {
   float top = s[0];
 #pragma unroll
   for (int i = 1; i < N; ++i) top = fmaxf(top, s[i]);
@@ -196,6 +197,7 @@ LVS_DEV void softmax_row(float (&s)[N], float& m, float& l, float c, bool first,
 #pragma unroll
   for (int i = 0; i < N; ++i) sum[i & 3] += s[i];
   l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  return top;
 }
 
 // Up to 16 query rows, on 16x16 tiles: a quarter of the wave's lanes (g4) holds a row (n16).
@@ -509,8 +511,8 @@ struct Segment {
 
   // softmax of a tile or piece; its mass on the video span
   template <int N, class KeyOf>
-  LVS_DEV void softmax(float (&s)[N], int key0, int keys, KeyOf&& key_of) {
-    softmax_row<Rows::kLanes>(s, st.m, st.l, p.scale_log2e, fresh, [&](float a) { st.rescale(a); });
+  LVS_DEV float softmax(float (&s)[N], int key0, int keys, KeyOf&& key_of) {
+    const float top = softmax_row<Rows::kLanes>(s, st.m, st.l, p.scale_log2e, fresh, [&](float a) { st.rescale(a); });
     fresh = false;
     if (key0 < vis_e && key0 + keys > vis_b) {
       float sum = 0.f;
@@ -521,6 +523,7 @@ struct Segment {
       }
       st.lv += sum;
     }
+    return top;
   }
 
   // tiles t0 .. t1-1 of a unit
