@@ -39,12 +39,11 @@ LVS_DEV f32x32 from_six(const Six& x, float scale) {
 
 // Sums of numbers of 6 bits at 2^e, 2^(e - 4), 2^(e - 9): what a term leaves, at most a quarter of its scale, is at most 4
 // of the second's, and what that leaves, an eighth, at most 4 of the third's.
-constexpr int kNext = 4;
 template <int N, class Put>
 LVS_DEV void split6(f32x16 x, f32x16 y, int e, Put&& put) {
 #pragma unroll
   for (int term = 0; term < N; ++term) {
-    const int at = e - kNext * term - (term == 2 ? 1 : 0);
+    const int at = e - 4 * term - (term == 2 ? 1 : 0);
     const float scale = __builtin_bit_cast(float, (uint32_t)(at + 127) << 23);
     const Six v = to_six(x, y, scale);
     put(term, v);
@@ -70,6 +69,10 @@ LVS_DEV f32x16 mfma_mx(const u32x4& a, uint32_t ks, const Six& b, uint32_t qs, c
 // 32 query rows on 32x32 tiles: the tokens of a lane's scores are those of its values, element 16 t + r is token
 // 32 t + 8 (r / 4) + 4 h + r % 4.
 struct FourRows : WideRows {
+  // A row of 32 tiles meets a new maximum in most of them, if only by a little, and a rescaling is a fifth of a tile's
+  // vector instructions: 4 x 65536 keys, 64 rows 87.4 -> 81.6 us, 16 x (2048 to 32768) keys 51.0 -> 48.5.  (Probabilities
+  // up to 2^8 are rounded as those up to 1 are; an exact 1 that the largest one often is otherwise is lost.)
+  static constexpr int kSlack = 8;
   static LVS_DEV int key_of(int lane, int e) { return 32 * (e >> 4) + 8 * ((e >> 2) & 3) + 4 * (lane >> 5) + (e & 3); }
   // channels 64 a + 32 h + 8 y .. +7 at 4 a + y, of queries and of open keys
   static LVS_DEV int channel(int x, int lane) { return 64 * (x >> 2) + 32 * (lane >> 5) + 8 * (x & 3); }
@@ -82,32 +85,54 @@ struct FourRows : WideRows {
     for (int x = 0; x < 8; ++x)
       k[x] = *reinterpret_cast<const u32x4*>(kt + ((p0 + (lane & 31)) & (kTailRows - 1)) * kRowBytes + 2 * channel(x, lane));
   }
+  static constexpr int kSplitChunks = 5;      // of 16 bytes a lane: three terms and scales of half of q
   Six q6[3][2];            // term, channels 64 a + 32 h .. + 31
   uint32_t qs[2];          // their scales' exponents, byte by term
 
-  // From q.  A row's 32 channels of which one is not finite are NaN.
-  LVS_DEV void split_q() {
+  // Half A of q to LDS, as lanes take it.  A row's 32 channels of which one is not finite are NaN.
+  template <int A>
+  LVS_DEV void split_q(uint32_t to, int lane) const {
+    uint32_t m = 0;
 #pragma unroll
-    for (int a = 0; a < 2; ++a) {
-      uint32_t m = 0;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const uint32_t w = q[4 * a + (i >> 2)][i & 3];
-        m = max(m, max(w & 0x7fffu, (w >> 16) & 0x7fffu));
-      }
-      const bool nan = m >= 0x7f80u;
-      const int e = max((int)(m >> 7) - 127 - 2 + ((m & 0x7fu) > 0x70u ? 1 : 0), -100);      // max |q| <= 7.5 * 2^e
-      f32x16 x, y;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const uint32_t w = nan ? 0u : q[4 * a + (i >> 2)][i & 3];
-        x[i] = __builtin_bit_cast(float, w << 16);
-        y[i] = __builtin_bit_cast(float, w & 0xffff0000u);
-      }
-      const uint32_t byte = (uint32_t)(e + 127);
-      qs[a] = nan ? 0xffffffffu : byte | ((byte - kNext) << 8) | ((byte - 2 * kNext - 1) << 16);
-      split6<3>(x, y, e, [&](int term, const Six& v) { q6[term][a] = v; });
+    for (int i = 0; i < 16; ++i) {
+      const uint32_t w = q[4 * A + (i >> 2)][i & 3];
+      m = max(m, max(w & 0x7fffu, (w >> 16) & 0x7fffu));
     }
+    const bool nan = m >= 0x7f80u;
+    const int e = max((int)(m >> 7) - 127 - 2 + ((m & 0x7fu) > 0x70u ? 1 : 0), -100);      // max |q| <= 7.5 * 2^e
+    f32x16 x, y;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const uint32_t w = nan ? 0u : q[4 * A + (i >> 2)][i & 3];
+      x[i] = __builtin_bit_cast(float, w << 16);
+      y[i] = __builtin_bit_cast(float, w & 0xffff0000u);
+    }
+    const uint32_t byte = (uint32_t)(e + 127);
+    uint32_t all[kSplitChunks * 4];
+    all[18] = nan ? 0xffffffffu : byte | ((byte - 4) << 8) | ((byte - 9) << 16);
+    all[19] = 0;
+    split6<3>(x, y, e, [&](int term, const Six& v) {
+#pragma unroll
+      for (int i = 0; i < 6; ++i) all[6 * term + i] = v[i];
+    });
+#pragma unroll
+    for (int i = 0; i < kSplitChunks; ++i)
+      *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(to + i * 1024 + lane * 16) =
+          u32x4{all[4 * i], all[4 * i + 1], all[4 * i + 2], all[4 * i + 3]};
+  }
+  template <int A>
+  LVS_DEV void take_q(uint32_t from, int lane) {
+    uint32_t all[kSplitChunks * 4];
+#pragma unroll
+    for (int i = 0; i < kSplitChunks; ++i) {
+      const u32x4 x = lds_load16(from + i * 1024 + lane * 16);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) all[4 * i + j] = x[j];
+    }
+#pragma unroll
+    for (int term = 0; term < 3; ++term) q6[term][A] = Six{all[6 * term], all[6 * term + 1], all[6 * term + 2],
+                                                           all[6 * term + 3], all[6 * term + 4], all[6 * term + 5]};
+    qs[A] = all[18];
   }
 
   LVS_DEV void scores4(float (&s)[32], const u32x4 (&k)[4], uint32_t scales) const {
@@ -153,7 +178,25 @@ struct Segment4 : Segment<FourRows, KS, ONCE> {
   using Base::stream;
   LVS_DEV Segment4(const PagedAttnKernelArgs& a, uint8_t* lds) : Base(a, lds) {}
 
-  // a lane's codes and scales of a tile's keys or values
+  const int32_t* row;                  // of the table
+  int h, t0, t1, mine;                 // kv head; tiles of the part; of the wave
+  int ids;                             // blocks of 64 of them, one per lane; -1: no block of the pool
+  int id;                              // of the tile that is on its way
+  int64_t at;                          // its place in the pools; where there is no block, the first's
+  u32x4 k[4];                          // its keys
+  uint32_t ks;
+
+  LVS_DEV void fetch(int j0, int lane) {
+    const int t = t0 + stream + KS * (j0 + lane);
+    ids = t < t1 ? row[t] : -1;
+    ids = (uint32_t)ids < (uint32_t)p.n_blocks ? ids : -1;
+  }
+  LVS_DEV void next(int j, int lane) {
+    if ((j & 63) == 0) fetch(j, lane);
+    id = __builtin_amdgcn_readlane(ids, j & 63);
+    at = (int64_t)max(id, 0) * p.Hkv + h;
+    load(k, ks, p.k8, p.k_scale, at, lane);
+  }
   LVS_DEV void load(u32x4 (&x)[4], uint32_t& scales, const uint8_t* pool, const void* scale, int64_t at, int lane) const {
     const uint8_t* from = pool + at * kPage4Bytes + (lane & 31) * 32 + (lane >> 5) * 16;
     scales = load_once<ONCE, uint32_t>(static_cast<const uint8_t*>(scale) + at * kScale4Bytes + lane * 4);
@@ -161,37 +204,34 @@ struct Segment4 : Segment<FourRows, KS, ONCE> {
     for (int i = 0; i < 4; ++i) x[i] = load_once<ONCE, u32x4>(from + i * 1024);
   }
 
-  // tiles t0 .. t1-1 of a unit
-  LVS_DEV void blocks4(int b, int h, int t0, int t1) {
-    const int mine = (t1 - t0 - stream + KS - 1) / KS;
-    if (mine <= 0) return;
+  // Tiles t0 .. t1-1 of a unit: the first one's loads, ahead of the open rows, ...
+  LVS_DEV void start4(int b, int head, int from, int to) {
+    row = p.table + (int64_t)b * p.cols;
+    h = head;
+    t0 = from;
+    t1 = to;
+    mine = (t1 - t0 - stream + KS - 1) / KS;
+    if (mine > 0) next(0, Base::lane_now());
+  }
+  // ... and what follows.  Two waves split the part's queries for all of them: for every wave by itself it is half a
+  // microsecond of each SIMD.
+  LVS_DEV void blocks4() {
+    if (t1 <= t0) return;
     const int lane = Base::lane_now();
-    const int32_t* row = p.table + (int64_t)b * p.cols;
-    int ids, id;                         // blocks of 64 tiles, one per lane; -1: no block of the pool
-    auto fetch = [&](int j0) {
-      const int t = t0 + stream + KS * (j0 + lane);
-      ids = t < t1 ? row[t] : -1;
-      ids = (uint32_t)ids < (uint32_t)p.n_blocks ? ids : -1;
-    };
-    auto place = [&](int j) {            // of the block in the pools; where there is none, of the first
-      if ((j & 63) == 0) fetch(j);
-      id = __builtin_amdgcn_readlane(ids, j & 63);
-      return (int64_t)max(id, 0) * p.Hkv + h;
-    };
-    st.split_q();
-    u32x4 k[4], v[4];
-    uint32_t ks, vs;
-    int64_t at = place(0);
-    load(k, ks, p.k8, p.k_scale, at, lane);
+    const uint32_t at0 = lds_addr(this->smem) + kPageBytes, at1 = at0 + kRingBytes;      // (behind open rows)
+    if (stream == 0) st.template split_q<0>(at0, lane);
+    if (stream == 1) st.template split_q<1>(at1, lane);
+    lds_barrier();
+    st.template take_q<0>(at0, lane);
+    st.template take_q<1>(at1, lane);
     for (int j = 0; j < mine; ++j) {
       const bool there = id >= 0;        // (an entry that names no block of the pool: no key)
+      u32x4 v[4];
+      uint32_t vs;
       load(v, vs, p.v8, p.v_scale, at, lane);
       float s[32];
       st.scores4(s, k, ks);
-      if (j + 1 < mine) {
-        at = place(j + 1);
-        load(k, ks, p.k8, p.k_scale, at, lane);
-      }
+      if (j + 1 < mine) next(j + 1, lane);
       if (!there) continue;
       this->softmax(s, (t0 + stream + KS * j) * kPageTokens, kPageTokens, [&](int e) { return FourRows::key_of(lane, e); });
       u32x4 pr[4];
@@ -215,7 +255,8 @@ __global__ __launch_bounds__(64 * KS, 2) void paged_mx_attn_kernel(PagedAttnKern
   const int L = o.p0 == 0 ? paged_len(p.kv_len[o.b], p.cols) : 0;      // (for the open rows)
   sg.begin(o.b, o.h, o.rc);
   if (o.p0 == 0) sg.open_rows(o.b, o.h, o.rc, L);
-  sg.blocks4(o.b, o.h, o.t0, o.t1);
+  sg.start4(o.b, o.h, o.t0, o.t1);
+  sg.blocks4();
   const uint32_t on = sg.active(o.t1 - o.t0, o.p0 == 0, L);
   if (o.n == 1)
     sg.finish(on, o.b, o.h, o.rc);
@@ -234,7 +275,8 @@ __global__ __launch_bounds__(64 * KS, 2) void paged_mx_attn_unit_kernel(PagedAtt
   const int L = paged_len(p.kv_len[b], p.cols);
   sg.begin(b, h, rc);
   sg.open_rows(b, h, rc, L);
-  sg.blocks4(b, h, 0, L >> kPageShift);
+  sg.start4(b, h, 0, L >> kPageShift);
+  sg.blocks4();
   sg.finish(sg.active(L >> kPageShift, true, L), b, h, rc);
 }
 

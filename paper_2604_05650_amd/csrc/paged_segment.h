@@ -177,14 +177,14 @@ LVS_DEV bool finite(float x) { return fabsf(x) <= 3.4028234663852886e38f; }
 // `first`: there is nothing to rescale yet.  The maximum is exact: a reference that is taken anew only for
 // scores 2^8 above it saves 1 to 4 % of the time and costs the exact 1 of the largest probability (error
 // against 64 bits 2.2e-3 -> 2.5e-3).
-// Returned: the lane's largest score, in base 2.
-template <int LANES, int N, class Rescale>
-LVS_DEV float softmax_row(float (&s)[N], float& m, float& l, float c, bool first, Rescale&& rescale) {
+// SLACK: what a score may be above the reference (in base 2) before the reference is taken anew.
+template <int LANES, int SLACK, int N, class Rescale>
+LVS_DEV void softmax_row(float (&s)[N], float& m, float& l, float c, bool first, Rescale&& rescale) {
   float top = s[0];
 #pragma unroll
   for (int i = 1; i < N; ++i) top = fmaxf(top, s[i]);
   top *= c;
-  if (__any(top > m)) {
+  if (__any(top > m + SLACK)) {
     float x = max_halves(fmaxf(m, top));
     if constexpr (LANES == 4) x = max_rows(x);
     const float alpha = fast_exp2(m - x);
@@ -197,13 +197,12 @@ LVS_DEV float softmax_row(float (&s)[N], float& m, float& l, float c, bool first
 #pragma unroll
   for (int i = 0; i < N; ++i) sum[i & 3] += s[i];
   l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-  return top;
 }
 
 // Up to 16 query rows, on 16x16 tiles: a quarter of the wave's lanes (g4) holds a row (n16).
 // A tile's scores: key 16 g4 + 4 kb + i is element 4 kb + i.
 struct Rows16 {
-  static constexpr int kRows = 16, kScores = 16, kLanes = 4;
+  static constexpr int kRows = 16, kScores = 16, kLanes = 4, kSlack = 0;
   u32x4 q[4];              // channels 64 (x/2) + 16 g4 + 8 (x%2) .. +7
   f32x4 acc[8];            // O^T: channels 16 db + 4 g4 + i
   float m, l, lv;
@@ -318,7 +317,7 @@ struct Rows16 {
 // (64 rows of a wave, which would share the conversion, take 400 registers, and half of a wave's are no operands
 // of its vector instructions: 16384 keys, 150 rows 29.1 us so, in chunks of 32 23.2; 8 x 8000, 64 rows 43.8 and 40.2.)
 struct WideRows {
-  static constexpr int kRows = 32, kScores = 32, kLanes = 2;
+  static constexpr int kRows = 32, kScores = 32, kLanes = 2, kSlack = 0;
   u32x4 q[8];              // channels 16 (2 (x/2) + h) + 8 (x%2) .. +7
   f32x16 acc[4];           // O^T: channels 32 db + 8 (r/4) + 4 h + r%4
   float m, l, lv;
@@ -511,8 +510,8 @@ struct Segment {
 
   // softmax of a tile or piece; its mass on the video span
   template <int N, class KeyOf>
-  LVS_DEV float softmax(float (&s)[N], int key0, int keys, KeyOf&& key_of) {
-    const float top = softmax_row<Rows::kLanes>(s, st.m, st.l, p.scale_log2e, fresh, [&](float a) { st.rescale(a); });
+  LVS_DEV void softmax(float (&s)[N], int key0, int keys, KeyOf&& key_of) {
+    softmax_row<Rows::kLanes, Rows::kSlack>(s, st.m, st.l, p.scale_log2e, fresh, [&](float a) { st.rescale(a); });
     fresh = false;
     if (key0 < vis_e && key0 + keys > vis_b) {
       float sum = 0.f;
@@ -523,7 +522,6 @@ struct Segment {
       }
       st.lv += sum;
     }
-    return top;
   }
 
   // tiles t0 .. t1-1 of a unit
