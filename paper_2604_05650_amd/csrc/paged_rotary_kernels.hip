@@ -6,6 +6,100 @@ namespace lvspec {
 
 namespace {
 
+// The packed rows of a tile and the blocks that end in it, as append_rows finds them, with the requests' first rows asked
+// for by all lanes at once.
+struct Tile {
+  const AppendKernelArgs& a;
+  const int t0, lane;
+  const RowPlace row;
+  int seq, begin, end;         // request of the lane's row, its packed rows; begin < 0: none
+  unsigned long long todo;     // last rows of blocks
+  int my_tail;                 // the ring's row for the lane's, -1: not, or later
+
+  LVS_DEV Tile(const AppendKernelArgs& args, int number)
+      : a(args), t0(number * kPageTokens), lane(threadIdx.x & 63), row(args, number * kPageTokens + (threadIdx.x & 63)) {
+    my_tail = row.to_tail && !row.later ? LVSPEC_SLOT_TAIL - row.slot : -1;
+    const bool last = row.slot >= 0 && (row.slot & (kPageTokens - 1)) == kPageTokens - 1 &&
+                      (row.slot >> kPageShift) < a.n_blocks;
+    todo = __ballot(last);
+    if (todo == 0ull) return;
+    seq = t0 + lane < a.n_rows ? a.row_seq[t0 + lane] : -1;
+    const bool ok = (uint32_t)seq < (uint32_t)a.B;
+    begin = ok ? a.cu_rows[seq] : -1;
+    end = ok ? a.cu_rows[seq + 1] : -1;
+    end = end < a.n_rows ? end : a.n_rows;
+    todo = __ballot(last && begin >= 0 && begin <= t0 + lane);
+  }
+  struct Block {
+    int at, id, p0, b, begin, end, row0;     // last row; place in the pool; position of its first row; request; rows
+  };
+  LVS_DEV bool next(Block& x) {
+    if (todo == 0ull) return false;
+    const int l = __builtin_ctzll(todo);
+    todo &= todo - 1;
+    x.at = t0 + l;
+    x.id = __builtin_amdgcn_readlane(row.slot, l) >> kPageShift;
+    x.p0 = __builtin_amdgcn_readlane(row.pos, l) - (kPageTokens - 1);
+    x.b = __builtin_amdgcn_readlane(seq, l);
+    x.begin = __builtin_amdgcn_readlane(begin, l);
+    x.end = __builtin_amdgcn_readlane(end, l);
+    x.row0 = x.at - (kPageTokens - 1);
+    return true;
+  }
+  // Ring rows of a block's request behind the block that are left to who reads its open rows: the first, and the i-th's
+  // ring row.
+  LVS_DEV int later_from(const Block& x) const { return max(x.at + 1, x.end - (kPageTokens - 1)); }
+  LVS_DEV int later_code(const Block& x, int64_t t) const {
+    const int s = t < x.end ? a.slots[t] : LVSPEC_SLOT_NONE;
+    return s <= LVSPEC_SLOT_TAIL && (LVSPEC_SLOT_TAIL - s) / kTailRows == x.b ? LVSPEC_SLOT_TAIL - s : -1;
+  }
+};
+
+// Values of a tile, heads first .. last-1, a head's rows asked for before the one before it is stored.
+template <class Pool>
+LVS_DEV void append_values(const AppendKernelArgs& a, typename Pool::Scratch& scratch, int number, int first, int last) {
+  Tile tile(a, number);
+  const int tid = threadIdx.x, q = tid >> 4, c = tid & 15;
+  auto ring = [&](int b, int h) { return a.v_tail + ((int64_t)b * a.Hkv + h) * (kTailRows * kRowBytes); };
+  auto to_ring = [&](int64_t t, int code) {
+    for (int h = first; h < last; ++h)
+      *reinterpret_cast<u32x4*>(ring(code / kTailRows, h) + code % kTailRows * kRowBytes + c * 16) =
+          *reinterpret_cast<const u32x4*>(a.v + t * a.v_sr + h * a.v_sh + c * 16);
+  };
+  if (__ballot(tile.my_tail >= 0) != 0ull) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int code = __shfl(tile.my_tail, 16 * i + q, 64);
+      if (code >= 0) to_ring(tile.t0 + 16 * i + q, code);
+    }
+  }
+  Tile::Block x;
+  while (tile.next(x)) {
+    u32x4 v[4];
+    auto load = [&](int h) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = 4 * q + i;
+        const uint8_t* from = x.row0 + r >= x.begin ? a.v + (int64_t)(x.row0 + r) * a.v_sr + h * a.v_sh
+                                                    : ring(x.b, h) + ((x.p0 + r) & (kTailRows - 1)) * kRowBytes;
+        v[i] = *reinterpret_cast<const u32x4*>(from + c * 16);
+      }
+    };
+    load(first);
+    for (int h = first; h < last; ++h) {
+      const u32x4 now[4] = {v[0], v[1], v[2], v[3]};
+      if (h + 1 < last) load(h + 1);
+      const int64_t to = (int64_t)x.id * a.Hkv + h;
+      if (Pool::store(now, true, a.v8, a.v_scale, to, scratch)) Pool::mend(a.v8, to);
+    }
+    if (x.row0 < x.begin)                                  // (the reads of the ring are behind a barrier)
+      for (int64_t t = tile.later_from(x) + q; t < x.end; t += kCacheThreads / 16) {
+        const int code = tile.later_code(x, t);
+        if (code >= 0) to_ring(t, code);
+      }
+  }
+}
+
 // Keys of a tile of 64 packed rows, heads first .. last-1.  Rotated rows are rounded to bf16, which is what the ring
 // holds, and go there or through LDS into their block: so a row's codes do not depend on the call it came in.
 // Thread (r, p) = (tid / 8, tid % 8) turns piece p, eight pairs, of rows r and r + 32; its cosines and sines serve all
@@ -25,13 +119,15 @@ struct RotatedKeys {
         e(piece_of(threadIdx.x & 7, 8, ro.half, 128, ro.interleaved != 0)) {}
 
   LVS_DEV void angles(int i, int64_t t) {
-    if (e.turned) turn[i].at(rot, t, 8 * p);
+    if (e.turned) turn[i].at(rot, t, e.f);
   }
-  // the thread's piece of a row, rotated where it is new
-  LVS_DEV void piece(Packed<__bf16, 8>& u, Packed<__bf16, 8>& v, int i, const uint8_t* row, bool is_new) const {
+  typedef Packed<__bf16, 8> Eight;
+  LVS_DEV void take(Eight& u, Eight& v, const uint8_t* row) const {
     u.load(reinterpret_cast<const __bf16*>(row) + e.a);
     v.load(reinterpret_cast<const __bf16*>(row) + e.b);
-    if (!is_new || !e.turned) return;
+  }
+  LVS_DEV void rotate(Eight& u, Eight& v, int i) const {
+    if (!e.turned) return;
     float x[8], y[8];
     u.get(x);
     v.get(y);
@@ -39,90 +135,87 @@ struct RotatedKeys {
     u.put(x);
     v.put(y);
   }
-  LVS_DEV void put(const Packed<__bf16, 8>& u, const Packed<__bf16, 8>& v, uint8_t* row) const {
+  LVS_DEV void put(const Eight& u, const Eight& v, uint8_t* row) const {
     u.store(reinterpret_cast<__bf16*>(row) + e.a);
     v.store(reinterpret_cast<__bf16*>(row) + e.b);
   }
-  // packed rows t[i] to ring rows code[i] (-1: not), in all the heads
+  // packed rows t[i] to ring rows code[i] (-1: not), in all the heads; a head's rows are asked for before the one before
+  // it, or the angles, are done
   LVS_DEV void to_ring(const int64_t (&t)[2], const int (&code)[2], int first, int last) {
+    Eight u[2], v[2];
+    auto load = [&](int h) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (code[i] >= 0) take(u[i], v[i], a.k + t[i] * a.k_sr + h * a.k_sh);
+    };
+    load(first);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
       if (code[i] >= 0) angles(i, t[i]);
-    for (int h = first; h < last; ++h)
+    for (int h = first; h < last; ++h) {
+      Eight x[2] = {u[0], u[1]}, y[2] = {v[0], v[1]};
+      if (h + 1 < last) load(h + 1);
 #pragma unroll
       for (int i = 0; i < 2; ++i)
         if (code[i] >= 0) {
-          Packed<__bf16, 8> u, v;
-          piece(u, v, i, a.k + t[i] * a.k_sr + h * a.k_sh, true);
-          put(u, v, a.k_tail + (((int64_t)(code[i] / kTailRows) * a.Hkv + h) * kTailRows + code[i] % kTailRows) * kRowBytes);
+          rotate(x[i], y[i], i);
+          put(x[i], y[i], a.k_tail + (((int64_t)(code[i] / kTailRows) * a.Hkv + h) * kTailRows + code[i] % kTailRows) * kRowBytes);
         }
+    }
   }
   LVS_DEV void tile(int number, int first, int last) {
-    const int tid = threadIdx.x, lane = tid & 63, q = tid >> 4, c = tid & 15;
-    const int t0 = number * kPageTokens, t = t0 + lane;
-    const RowPlace row(a, t);
-    const int my_tail = row.to_tail && !row.later ? LVSPEC_SLOT_TAIL - row.slot : -1;
-    if (__ballot(my_tail >= 0) != 0ull) {
-      const int64_t at[2] = {t0 + r, t0 + r + 32};
-      const int code[2] = {__shfl(my_tail, r, 64), __shfl(my_tail, r + 32, 64)};
+    Tile tile(a, number);
+    const int tid = threadIdx.x, q = tid >> 4, c = tid & 15;
+    if (__ballot(tile.my_tail >= 0) != 0ull) {
+      const int64_t at[2] = {tile.t0 + r, tile.t0 + r + 32};
+      const int code[2] = {__shfl(tile.my_tail, r, 64), __shfl(tile.my_tail, r + 32, 64)};
       to_ring(at, code, first, last);
     }
-    unsigned long long todo = __ballot(row.slot >= 0 && (row.slot & (kPageTokens - 1)) == kPageTokens - 1);
-    while (todo != 0ull) {
-      const int l = __builtin_ctzll(todo);
-      todo &= todo - 1;
-      const int at = t0 + l;                               // last row of the block
-      const int id = __builtin_amdgcn_readlane(row.slot, l) >> kPageShift;
-      const int p0 = __builtin_amdgcn_readlane(row.pos, l) - (kPageTokens - 1);
-      const int b = a.row_seq[at];
-      if (id >= a.n_blocks || (uint32_t)b >= (uint32_t)a.B) continue;
-      const int begin = a.cu_rows[b];
-      if (begin < 0 || begin > at) continue;
-      const int row0 = at - (kPageTokens - 1);
+    Tile::Block b;
+    while (tile.next(b)) {
+      Eight u[2], v[2];
       bool is_new[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        is_new[i] = row0 + r + 32 * i >= begin;
-        if (is_new[i]) angles(i, row0 + r + 32 * i);
-      }
-      for (int h = first; h < last; ++h) {
-        const uint8_t* ring = a.k_tail + ((int64_t)b * a.Hkv + h) * (kTailRows * kRowBytes);
-        Packed<__bf16, 8> u[2], v[2];
+      auto load = [&](int h) {
+        const uint8_t* ring = a.k_tail + ((int64_t)b.b * a.Hkv + h) * (kTailRows * kRowBytes);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int k = r + 32 * i;
-          piece(u[i], v[i], i, is_new[i] ? a.k + (int64_t)(row0 + k) * a.k_sr + h * a.k_sh
-                                         : ring + ((p0 + k) & (kTailRows - 1)) * kRowBytes, is_new[i]);
+          take(u[i], v[i], is_new[i] ? a.k + (int64_t)(b.row0 + k) * a.k_sr + h * a.k_sh
+                                     : ring + ((b.p0 + k) & (kTailRows - 1)) * kRowBytes);
         }
-        __syncthreads();                                   // (the rows of the head before this one have been read)
+      };
 #pragma unroll
-        for (int i = 0; i < 2; ++i) put(u[i], v[i], s_rows + (r + 32 * i) * kRowBytes);
-        __syncthreads();
+      for (int i = 0; i < 2; ++i) is_new[i] = b.row0 + r + 32 * i >= b.begin;
+      load(first);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (is_new[i]) angles(i, b.row0 + r + 32 * i);
+      for (int h = first; h < last; ++h) {
+        // (the rows of the head before this one have been read: there are barriers behind that in store)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if (is_new[i]) rotate(u[i], v[i], i);
+          put(u[i], v[i], s_rows + (r + 32 * i) * kRowBytes);
+        }
+        if (h + 1 < last) load(h + 1);
+        lds_barrier();
         u32x4 x[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const u32x4*>(s_rows + (4 * q + i) * kRowBytes + c * 16);
-        const int64_t to = (int64_t)id * a.Hkv + h;
+        const int64_t to = (int64_t)b.id * a.Hkv + h;
         if (Pool::store(x, false, a.k8, a.k_scale, to, scratch)) Pool::mend(a.k8, to);
       }
-      if (row0 < begin) {                                  // (the reads of the ring are behind a barrier)
-        int end = a.cu_rows[b + 1];
-        end = end < a.n_rows ? end : a.n_rows;
-        const int from = max(at + 1, end - (kPageTokens - 1));
-        int64_t rows[2];
-        int code[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          rows[i] = from + r + 32 * i;
-          const int s = rows[i] < end ? a.slots[rows[i]] : LVSPEC_SLOT_NONE;
-          code[i] = s <= LVSPEC_SLOT_TAIL && (LVSPEC_SLOT_TAIL - s) / kTailRows == b ? LVSPEC_SLOT_TAIL - s : -1;
-        }
+      if (b.row0 < b.begin) {                              // (the reads of the ring are behind a barrier)
+        const int from = tile.later_from(b);
+        const int64_t rows[2] = {from + r, from + r + 32};
+        const int code[2] = {tile.later_code(b, rows[0]), tile.later_code(b, rows[1])};
         to_ring(rows, code, first, last);
       }
     }
   }
 };
 
-// Workgroups: keys by tile and group of heads, values by tile and head, queries by 256 pieces and group of heads.
+// Workgroups: keys by tile and group of heads, values the same, queries by 256 pieces and group of heads.
 template <class Pool>
 __global__ __launch_bounds__(kCacheThreads) void paged_append_rotary_kernel(AppendRotaryKernelArgs a) {
   __shared__ typename Pool::Scratch scratch;
@@ -136,12 +229,12 @@ __global__ __launch_bounds__(kCacheThreads) void paged_append_rotary_kernel(Appe
     return;
   }
   w -= tiles * a.k_groups;
-  if (w < tiles * a.rows.Hkv) {
-    const int h = w / tiles;
-    append_rows<Pool>(a.rows, scratch, w - h * tiles, h, true);
+  if (w < tiles * a.k_groups) {
+    const int group = w / tiles, first = group * a.k_heads;
+    append_values<Pool>(a.rows, scratch, w - group * tiles, first, min(first + a.k_heads, a.rows.Hkv));
     return;
   }
-  w -= tiles * a.rows.Hkv;
+  w -= tiles * a.k_groups;
   const int group = w / a.q_wgs;
   const int64_t i = (int64_t)(w - group * a.q_wgs) * kCacheThreads + threadIdx.x, t = i >> 3;
   if (t >= a.rows.n_rows || a.rows.row_seq[t] < 0) return;
@@ -149,19 +242,20 @@ __global__ __launch_bounds__(kCacheThreads) void paged_append_rotary_kernel(Appe
   const Piece e = piece_of((int)i & 7, 8, a.rot.half, 128, pairs);
   if (!e.turned && a.q.x == a.q.y) return;
   Turn<8> turn;
-  if (e.turned) turn.at(a.rot, t, 8 * ((int)i & 7));
+  if (e.turned) turn.at(a.rot, t, e.f);
   rotate_heads<__bf16, 8>(a.q, turn, e, pairs, t, group * a.q_heads, min((group + 1) * a.q_heads, a.q.H));
 }
 
 template <class Pool>
 hipError_t launch(AppendRotaryKernelArgs a, hipStream_t stream) {
   const int64_t tiles = (a.rows.n_rows + kPageTokens - 1) / kPageTokens, cus = num_compute_units();
-  // keys: heads that share a row's angles, as many as leave two workgroups for a compute unit
-  int64_t k_groups = (2 * cus + tiles - 1) / tiles;
+  // Heads that share a row's angles: as many as leave a workgroup of keys for each compute unit.  16384 rows, 8 heads,
+  // 256 tiles: one group 28.0 us, two 31.9, four 39.9.
+  int64_t k_groups = (cus + tiles - 1) / tiles;
   k_groups = k_groups > a.rows.Hkv ? a.rows.Hkv : k_groups;
   a.k_heads = (int)((a.rows.Hkv + k_groups - 1) / k_groups);
   a.k_groups = (a.rows.Hkv + a.k_heads - 1) / a.k_heads;
-  int64_t wgs = tiles * (a.k_groups + a.rows.Hkv);
+  int64_t wgs = tiles * 2 * a.k_groups;
   if (a.q.H > 0) {
     const int64_t threads = (int64_t)a.rows.n_rows * 8;
     a.q_wgs = (int)((threads + kCacheThreads - 1) / kCacheThreads);

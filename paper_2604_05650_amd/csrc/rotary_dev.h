@@ -40,16 +40,18 @@ LVS_DEV void cos_sin(double a, double& c, double& s) {
   if (quarter >= 2) s = -s;
 }
 
-// Cosines and sines of W frequencies from f0 on, for packed row t.
+// Cosines and sines of a piece's W frequencies (Piece), for packed row t.
 template <int W>
 struct Turn {
   double c[W], s[W];
   LVS_DEV void at(const RotaryKernelArgs& r, int64_t t, int f0) {
     const int first = r.axis != nullptr ? 0 : r.pos[t];
+    const int jump = W > 1 && r.interleaved != 0 ? (r.half - W) / 2 : 0;
 #pragma unroll
     for (int j = 0; j < W; ++j) {
-      const int pos = r.axis != nullptr ? r.pos[(int64_t)min((int)r.axis[f0 + j], r.n_axes - 1) * r.pos_sa + t] : first;
-      cos_sin((double)pos * (double)r.inv_freq[f0 + j], c[j], s[j]);      // (the product is exact up to 2^29)
+      const int f = f0 + j + (j >= W / 2 ? jump : 0);
+      const int pos = r.axis != nullptr ? r.pos[(int64_t)min((int)r.axis[f], r.n_axes - 1) * r.pos_sa + t] : first;
+      cos_sin((double)pos * (double)r.inv_freq[f], c[j], s[j]);      // (the product is exact up to 2^29)
       c[j] *= r.factor;
       s[j] *= r.sine;
     }
@@ -62,12 +64,10 @@ struct Turn {
       x = (float)__builtin_fma(u, c[j], -(v * s[j]));
       y = (float)__builtin_fma(v, c[j], u * s[j]);
     };
-    if (!pairs) {
+    if (!pairs || W == 1) {
 #pragma unroll
       for (int j = 0; j < W; ++j) one(a[j], b[j], j);
-    } else if constexpr (W == 1) {
-      one(a[0], b[0], 0);
-    } else {
+    } else if constexpr (W > 1) {
 #pragma unroll
       for (int j = 0; j < W / 2; ++j) {
         one(a[2 * j], a[2 * j + 1], j);
@@ -102,38 +102,51 @@ struct Packed<T, 1> {
   LVS_DEV void put(const float (&f)[1]) { x = (T)f[0]; }
 };
 
-// What a thread has of a head's channels: W at a and W at b.  Piece p of a row is its pairs p W .. p W + W - 1; pieces
-// behind them are 2 W channels that stay as they are (the last one W where their number is odd).
+// What a thread has of a head's channels: W at a and W at b, far enough apart that the threads of a row read in one
+// piece.  Turned are pieces p < half / W: channels p W and half + p W, which are pairs, or whose
+// neighbours are (W = 1: the two neighbours).  Pieces
+// behind them stay as they are (the last one W channels, where their number is odd).
 struct Piece {
   int a, b;                // channels; b < 0: none
+  int f;                   // first frequency (of the second W / 2 neighbours half / 2 further on)
   bool turned;
 };
 LVS_DEV Piece piece_of(int p, int W, int half, int D, bool pairs) {
-  if (p * W < half) return pairs ? Piece{2 * p * W, 2 * p * W + W, true} : Piece{p * W, half + p * W, true};
-  const int at = 2 * half + 2 * W * (p - half / W);
-  return Piece{at, at + W < D ? at + W : -1, false};
+  if (W == 1 && pairs && p < half) return Piece{2 * p, 2 * p + 1, p, true};
+  if (p * W < half) return Piece{p * W, half + p * W, pairs ? p * W / 2 : p * W, true};
+  const int rest = (D - 2 * half) / W, at = p - half / W, b = at + (rest + 1) / 2;
+  return Piece{2 * half + at * W, b < rest ? 2 * half + b * W : -1, 0, false};
 }
 inline int pieces(int W, int half, int D) { return half / W + ((D - 2 * half) / W + 1) / 2; }
 
-// A thread's piece of row t in the heads first .. last-1 of a tensor.
+// A thread's piece of row t in the heads first .. last-1 of a tensor: loads of kAhead heads at a time.
+constexpr int kAhead = 4;
 template <class T, int W>
 LVS_DEV void rotate_heads(const RotaryRows& x, const Turn<W>& turn, const Piece& e, bool pairs, int64_t t, int first, int last) {
   const T* from = static_cast<const T*>(x.x) + t * x.x_sr;
   T* to = static_cast<T*>(x.y) + t * x.y_sr;
-  for (int h = first; h < last; ++h) {
-    Packed<T, W> u, v;
-    u.load(from + h * x.x_sh + e.a);
-    if (e.b >= 0) v.load(from + h * x.x_sh + e.b);
-    if (e.turned) {
-      float a[W], b[W];
-      u.get(a);
-      v.get(b);
-      turn.apply(a, b, pairs);
-      u.put(a);
-      v.put(b);
-    }
-    u.store(to + h * x.y_sh + e.a);
-    if (e.b >= 0) v.store(to + h * x.y_sh + e.b);
+  for (int h0 = first; h0 < last; h0 += kAhead) {
+    Packed<T, W> u[kAhead], v[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (h0 + i < last) {
+        u[i].load(from + (h0 + i) * x.x_sh + e.a);
+        if (e.b >= 0) v[i].load(from + (h0 + i) * x.x_sh + e.b);
+      }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (h0 + i < last) {
+        if (e.turned) {
+          float a[W], b[W];
+          u[i].get(a);
+          v[i].get(b);
+          turn.apply(a, b, pairs);
+          u[i].put(a);
+          v[i].put(b);
+        }
+        u[i].store(to + (h0 + i) * x.y_sh + e.a);
+        if (e.b >= 0) v[i].store(to + (h0 + i) * x.y_sh + e.b);
+      }
   }
 }
 

@@ -21,7 +21,7 @@ __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryCallArgs a
   if (!e.turned && a.in_place) return;
   const int h0 = blockIdx.y * a.heads, h1 = h0 + a.heads;
   Turn<W> turn;
-  if (e.turned) turn.at(a.rot, t, p * W);
+  if (e.turned) turn.at(a.rot, t, e.f);
   rotate_heads<T, W>(a.q, turn, e, pairs, t, min(h0, a.q.H), min(h1, a.q.H));
   if (a.k.H > 0) rotate_heads<T, W>(a.k, turn, e, pairs, t, max(h0 - a.q.H, 0), min(max(h1 - a.q.H, 0), a.k.H));
 }
