@@ -238,12 +238,11 @@ __global__ __launch_bounds__(kCacheThreads) void paged_append_rotary_kernel(Appe
   const int group = w / a.q_wgs;
   const int64_t i = (int64_t)(w - group * a.q_wgs) * kCacheThreads + threadIdx.x, t = i >> 3;
   if (t >= a.rows.n_rows || a.rows.row_seq[t] < 0) return;
-  const bool pairs = a.rot.interleaved != 0;
-  const Piece e = piece_of((int)i & 7, 8, a.rot.half, 128, pairs);
+  const Piece e = piece_of((int)i & 7, 8, a.rot.half, 128, a.rot.interleaved != 0);
   if (!e.turned && a.q.x == a.q.y) return;
   Turn<8> turn;
-  if (e.turned) turn.at(a.rot, t, e.f);
-  rotate_heads<__bf16, 8>(a.q, turn, e, pairs, t, group * a.q_heads, min((group + 1) * a.q_heads, a.q.H));
+  bool ready = false;
+  rotate_heads<__bf16, 8>(a.q, a.rot, turn, ready, e, t, group * a.q_heads, min((group + 1) * a.q_heads, a.q.H));
 }
 
 template <class Pool>

@@ -119,10 +119,13 @@ LVS_DEV Piece piece_of(int p, int W, int half, int D, bool pairs) {
 }
 inline int pieces(int W, int half, int D) { return half / W + ((D - 2 * half) / W + 1) / 2; }
 
-// A thread's piece of row t in the heads first .. last-1 of a tensor: loads of kAhead heads at a time.
+// A thread's piece of row t in the heads first .. last-1 of a tensor: loads of kAhead heads at a time, the first of them
+// ahead of the angles, where those are not `ready`.
 constexpr int kAhead = 4;
 template <class T, int W>
-LVS_DEV void rotate_heads(const RotaryRows& x, const Turn<W>& turn, const Piece& e, bool pairs, int64_t t, int first, int last) {
+LVS_DEV void rotate_heads(const RotaryRows& x, const RotaryKernelArgs& r, Turn<W>& turn, bool& ready, const Piece& e,
+                          int64_t t, int first, int last) {
+  const bool pairs = r.interleaved != 0;
   const T* from = static_cast<const T*>(x.x) + t * x.x_sr;
   T* to = static_cast<T*>(x.y) + t * x.y_sr;
   for (int h0 = first; h0 < last; h0 += kAhead) {
@@ -133,6 +136,8 @@ LVS_DEV void rotate_heads(const RotaryRows& x, const Turn<W>& turn, const Piece&
         u[i].load(from + (h0 + i) * x.x_sh + e.a);
         if (e.b >= 0) v[i].load(from + (h0 + i) * x.x_sh + e.b);
       }
+    if (e.turned && !ready) turn.at(r, t, e.f);
+    ready = true;
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
       if (h0 + i < last) {

@@ -15,15 +15,14 @@ __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryCallArgs a
   const int64_t i = (int64_t)blockIdx.x * kRotaryThreads + threadIdx.x;
   const int64_t t = i / a.pieces;
   if (t >= a.n_rows) return;
-  const bool pairs = a.rot.interleaved != 0;
-  const int p = (int)(i - t * a.pieces);
-  const Piece e = piece_of(p, W, a.rot.half, a.D, pairs);
+  const Piece e = piece_of((int)(i - t * a.pieces), W, a.rot.half, a.D, a.rot.interleaved != 0);
   if (!e.turned && a.in_place) return;
   const int h0 = blockIdx.y * a.heads, h1 = h0 + a.heads;
   Turn<W> turn;
-  if (e.turned) turn.at(a.rot, t, e.f);
-  rotate_heads<T, W>(a.q, turn, e, pairs, t, min(h0, a.q.H), min(h1, a.q.H));
-  if (a.k.H > 0) rotate_heads<T, W>(a.k, turn, e, pairs, t, max(h0 - a.q.H, 0), min(max(h1 - a.q.H, 0), a.k.H));
+  bool ready = false;
+  rotate_heads<T, W>(a.q, a.rot, turn, ready, e, t, min(h0, a.q.H), min(h1, a.q.H));
+  if (a.k.H > 0)
+    rotate_heads<T, W>(a.k, a.rot, turn, ready, e, t, max(h0 - a.q.H, 0), min(max(h1 - a.q.H, 0), a.k.H));
 }
 
 template <class T, int W>
