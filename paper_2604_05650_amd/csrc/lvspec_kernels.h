@@ -289,7 +289,7 @@ struct AppendRotaryKernelArgs {
   AppendKernelArgs rows;
   RotaryKernelArgs rot;
   RotaryRows q;
-  int k_heads, k_groups, q_heads, q_wgs;    // (of the launch)
+  int k_heads, k_groups, v_heads, v_groups, q_heads, q_wgs;    // (of the launch)
 };
 hipError_t launch_paged_append_rotary(const AppendRotaryKernelArgs& a, bool four, hipStream_t stream);
 

@@ -215,7 +215,7 @@ struct RotatedKeys {
   }
 };
 
-// Workgroups: keys by tile and group of heads, values the same, queries by 256 pieces and group of heads.
+// Workgroups: keys, and values, by tile and group of heads, queries by 256 pieces and group of heads.
 template <class Pool>
 __global__ __launch_bounds__(kCacheThreads) void paged_append_rotary_kernel(AppendRotaryKernelArgs a) {
   __shared__ typename Pool::Scratch scratch;
@@ -229,12 +229,12 @@ __global__ __launch_bounds__(kCacheThreads) void paged_append_rotary_kernel(Appe
     return;
   }
   w -= tiles * a.k_groups;
-  if (w < tiles * a.k_groups) {
-    const int group = w / tiles, first = group * a.k_heads;
-    append_values<Pool>(a.rows, scratch, w - group * tiles, first, min(first + a.k_heads, a.rows.Hkv));
+  if (w < tiles * a.v_groups) {
+    const int group = w / tiles, first = group * a.v_heads;
+    append_values<Pool>(a.rows, scratch, w - group * tiles, first, min(first + a.v_heads, a.rows.Hkv));
     return;
   }
-  w -= tiles * a.k_groups;
+  w -= tiles * a.v_groups;
   const int group = w / a.q_wgs;
   const int64_t i = (int64_t)(w - group * a.q_wgs) * kCacheThreads + threadIdx.x, t = i >> 3;
   if (t >= a.rows.n_rows || a.rows.row_seq[t] < 0) return;
@@ -254,7 +254,12 @@ hipError_t launch(AppendRotaryKernelArgs a, hipStream_t stream) {
   k_groups = k_groups > a.rows.Hkv ? a.rows.Hkv : k_groups;
   a.k_heads = (int)((a.rows.Hkv + k_groups - 1) / k_groups);
   a.k_groups = (a.rows.Hkv + a.k_heads - 1) / a.k_heads;
-  int64_t wgs = tiles * 2 * a.k_groups;
+  // Values have no angles to share, but two workgroups are all that a compute unit has room for: four heads.  16384 rows,
+  // 8 heads eight 27.8 us, four 27.0, two 28.9, one 31.3; 12 x (300 to 9000) rows in 4 bits, read back too, eight 89.1,
+  // four 81.1, two 80.1, one 85.4.
+  a.v_heads = a.k_heads < 4 ? a.k_heads : 4;
+  a.v_groups = (a.rows.Hkv + a.v_heads - 1) / a.v_heads;
+  int64_t wgs = tiles * (a.k_groups + a.v_groups);
   if (a.q.H > 0) {
     const int64_t threads = (int64_t)a.rows.n_rows * 8;
     a.q_wgs = (int)((threads + kCacheThreads - 1) / kCacheThreads);
