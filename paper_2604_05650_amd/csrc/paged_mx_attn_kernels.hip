@@ -37,18 +37,17 @@ LVS_DEV f32x32 from_six(const Six& x, float scale) {
   return r;
 }
 
-// Sums of numbers of 6 bits at 2^e, 2^(e - 4), 2^(e - 9): what a term leaves, at most a quarter of its scale, is at most 4
-// of the second's, and what that leaves, an eighth, at most 4 of the third's.
-template <int N, class Put>
-LVS_DEV void split6(f32x16 x, f32x16 y, int e, Put&& put) {
+// Three terms, at scales of 1, 2^-4 and 2^-9, of numbers up to 7.5: what a term leaves, at most a quarter of its scale, is
+// at most 4 of the second's, and what that leaves, an eighth, at most 4 of the third's.
+template <class Put>
+LVS_DEV void split6(f32x16 x, f32x16 y, Put&& put) {
+  constexpr float kScale[3] = {1.f, 0x1p-4f, 0x1p-9f};
 #pragma unroll
-  for (int term = 0; term < N; ++term) {
-    const int at = e - 4 * term - (term == 2 ? 1 : 0);
-    const float scale = __builtin_bit_cast(float, (uint32_t)(at + 127) << 23);
-    const Six v = to_six(x, y, scale);
+  for (int term = 0; term < 3; ++term) {
+    const Six v = to_six(x, y, kScale[term]);
     put(term, v);
-    if (term + 1 < N) {
-      const f32x32 z = from_six(v, scale);
+    if (term < 2) {
+      const f32x32 z = from_six(v, kScale[term]);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         x[i] -= z[2 * i];
@@ -100,18 +99,19 @@ struct FourRows : WideRows {
     }
     const bool nan = m >= 0x7f80u;
     const int e = max((int)(m >> 7) - 127 - 2 + ((m & 0x7fu) > 0x70u ? 1 : 0), -100);      // max |q| <= 7.5 * 2^e
+    const float inv = __builtin_bit_cast(float, (uint32_t)(127 - e) << 23);
     f32x16 x, y;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const uint32_t w = nan ? 0u : q[4 * A + (i >> 2)][i & 3];
-      x[i] = __builtin_bit_cast(float, w << 16);
-      y[i] = __builtin_bit_cast(float, w & 0xffff0000u);
+      x[i] = __builtin_bit_cast(float, w << 16) * inv;      // (at 2^126 the nearest of 6 bits may be 2^128)
+      y[i] = __builtin_bit_cast(float, w & 0xffff0000u) * inv;
     }
     const uint32_t byte = (uint32_t)(e + 127);
     uint32_t all[kSplitChunks * 4];
     all[18] = nan ? 0xffffffffu : byte | ((byte - 4) << 8) | ((byte - 9) << 16);
     all[19] = 0;
-    split6<3>(x, y, e, [&](int term, const Six& v) {
+    split6(x, y, [&](int term, const Six& v) {
 #pragma unroll
       for (int i = 0; i < 6; ++i) all[6 * term + i] = v[i];
     });

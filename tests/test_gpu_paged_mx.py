@@ -291,6 +291,45 @@ def test_scores_far_below_any_usual_one(L, n, spare_cols):  # noqa: F811
         assert bool(((s + 2.0 ** 113 * least).abs() <= 2.0 ** 113 * least * 2.0 ** -21).all())
 
 
+@pytest.mark.parametrize("spare_cols", [1, 70])
+def test_queries_of_any_size(L, spare_cols):  # noqa: F811
+    """Rows from bf16's smallest to its largest numbers, with channels of every size beside each other, where the score
+    scale brings them back; and a row that is not finite is NaN, the others are what they are without it.
+
+    Keys here are powers of two on one channel a token, so that a score is one product: queries within 2^-7 of their 32's
+    largest go into it exactly, smaller ones with 2^-15 of that largest at most, which is below 2^-12 for scores up to 8."""
+    kv, g, H = [130, 700], 4, 2
+    cache, table = ready_mx(L, 970, 2, H, kv, spare_cols=spare_cols)
+    cache.k_pool.zero_()
+    cache.k_scale.fill_(127)
+    one = torch.arange(64, device=DEV)
+    cache.k_pool[:, :, 0, one, one % 32] = 0x02                                # code of 1 on channel 2 (t % 32), first half
+    cache.k_tail.zero_()
+    for p in range(RING):
+        cache.k_tail[:, :, p, 2 * (p % 64 % 32)] = 1.0
+    base = normal(971, (2, g, 4, D))
+    base = base.clamp(-4, 4)
+    base[:, :, 1] *= torch.logspace(-6, 0, D, device=DEV).to(torch.bfloat16)   # channels of very different sizes
+    for e, scale in ((0, 1.0), (100, 2.0 ** -100), (-100, 0.0), (125, 2.0 ** -125)):
+        q = (base.float() * 2.0 ** e).to(torch.bfloat16) if e != 125 else (base.float().clamp(-3.98, 3.98) * 2.0 ** 126).to(torch.bfloat16)
+        out, lse, _ = L.verify_attn_paged_mx(q, cache, i32(table), i32(kv), scale=scale, return_lse=True)
+        ro, rl, _, size = M.attention(q.double().cpu().numpy(), M.as_numpy(cache), table, kv, None, scale if scale > 0 else None)
+        o = out.double().cpu().numpy()
+        assert np.all(np.isfinite(o))
+        # a score off by d moves a probability by its d-th part: 2^-12, beside the two roundings to bf16
+        assert np.all(np.abs(o - ro) <= (1.02 * 2.0 ** -8 + 2.0 ** -11) * (size + np.abs(ro)) + 1e-30), e
+        assert np.all(np.abs(lse.cpu().numpy() - rl) <= 2.0 ** -12 + 2e-5 * (1 + np.abs(rl))), e
+    want, wl, _ = L.verify_attn_paged_mx(base, cache, i32(table), i32(kv), return_lse=True)
+    for value in (float("nan"), float("inf"), float("-inf")):
+        q = base.clone()
+        q[1, 2, 3, 77] = value
+        got, gl, _ = L.verify_attn_paged_mx(q, cache, i32(table), i32(kv), return_lse=True)
+        hit = torch.zeros(got.shape, dtype=torch.bool, device=DEV)
+        hit[1, 2, 3] = True
+        assert bool(torch.isnan(got[hit]).all()) and torch.equal(got[~hit], want[~hit])
+        assert bool(torch.isnan(gl[1, 3, 2])) and torch.equal(gl[0], wl[0])
+
+
 def test_attention_over_the_largest_values(L):  # noqa: F811
     """Equal weights over one block of the largest numbers: their mean is finite."""
     cache = L.alloc_paged_mx_cache(1, 1, 1, DEV)
