@@ -69,8 +69,8 @@ LVS_DEV f32x16 mfma_mx(const u32x4& a, uint32_t ks, const Six& b, uint32_t qs, c
 // 32 t + 8 (r / 4) + 4 h + r % 4.
 struct FourRows : WideRows {
   // A row of 32 tiles meets a new maximum in most of them, if only by a little, and a rescaling is a fifth of a tile's
-  // vector instructions: 4 x 65536 keys, 64 rows 87.4 -> 81.6 us, 16 x (2048 to 32768) keys 51.0 -> 48.5.  (Probabilities
-  // up to 2^8 are rounded as those up to 1 are; an exact 1 that the largest one often is otherwise is lost.)
+  // vector instructions: 4 x 65536 keys, 64 rows 87.4 -> 81.6 us, 16 x (2048 to 32768) keys 51.0 -> 48.5.  (The exact 1
+  // that the largest probability often is otherwise is lost.)
   static constexpr int kSlack = 8;
   static LVS_DEV int key_of(int lane, int e) { return 32 * (e >> 4) + 8 * ((e >> 2) & 3) + 4 * (lane >> 5) + (e & 3); }
   // channels 64 a + 32 h + 8 y .. +7 at 4 a + y, of queries and of open keys
@@ -98,7 +98,7 @@ struct FourRows : WideRows {
       m = max(m, max(w & 0x7fffu, (w >> 16) & 0x7fffu));
     }
     const bool nan = m >= 0x7f80u;
-    const int e = max((int)(m >> 7) - 127 - 2 + ((m & 0x7fu) > 0x70u ? 1 : 0), -100);      // max |q| <= 7.5 * 2^e
+    const int e = max((int)(m >> 7) - 127 - 2 + ((m & 0x7fu) > 0x70u ? 1 : 0), -118);      // max |q| <= 7.5 * 2^e; 2^(e-9) is a scale
     const float inv = __builtin_bit_cast(float, (uint32_t)(127 - e) << 23);
     f32x16 x, y;
 #pragma unroll

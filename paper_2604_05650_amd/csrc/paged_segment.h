@@ -174,18 +174,19 @@ LVS_DEV f32x4 four_bf16(const uint8_t* at) {
 LVS_DEV bool finite(float x) { return fabsf(x) <= 3.4028234663852886e38f; }
 
 // Scores of a tile to probabilities (in place); running maximum m, sum l.  LANES lanes hold a row's scores.
-// `first`: there is nothing to rescale yet.  The maximum is exact: a reference that is taken anew only for
-// scores 2^8 above it saves 1 to 4 % of the time and costs the exact 1 of the largest probability (error
+// `first`: there is nothing to rescale yet.  The cache in 8 bits keeps the exact maximum: a reference that is taken anew
+// only for scores 2^8 above it saves 1 to 4 % of the time there and costs the exact 1 of the largest probability (error
 // against 64 bits 2.2e-3 -> 2.5e-3).
-// SLACK: what a score may be above the reference (in base 2) before the reference is taken anew.
+// SLACK: how far (in base 2) the reference is put above the largest score when it is taken anew, which is when a score
+// is above it.  No probability is above 1: sums over large values overflow no sooner than with the exact maximum.
 template <int LANES, int SLACK, int N, class Rescale>
 LVS_DEV void softmax_row(float (&s)[N], float& m, float& l, float c, bool first, Rescale&& rescale) {
   float top = s[0];
 #pragma unroll
   for (int i = 1; i < N; ++i) top = fmaxf(top, s[i]);
   top *= c;
-  if (__any(top > m + SLACK)) {
-    float x = max_halves(fmaxf(m, top));
+  if (__any(top > m)) {
+    float x = max_halves(fmaxf(m, top + SLACK));
     if constexpr (LANES == 4) x = max_rows(x);
     const float alpha = fast_exp2(m - x);
     m = x;

@@ -310,8 +310,11 @@ def test_queries_of_any_size(L, spare_cols):  # noqa: F811
     base = normal(971, (2, g, 4, D))
     base = base.clamp(-4, 4)
     base[:, :, 1] *= torch.logspace(-6, 0, D, device=DEV).to(torch.bfloat16)   # channels of very different sizes
-    for e, scale in ((0, 1.0), (100, 2.0 ** -100), (-100, 0.0), (125, 2.0 ** -125)):
+    for e, scale, keys in ((0, 1.0, 0), (100, 2.0 ** -100, 0), (-100, 0.0, 0), (-100, 1.0, 100), (-115, 1.0, 115), (125, 2.0 ** -125, 0)):
+        cache.k_scale.fill_(127 + keys)
+        cache.k_tail.copy_(torch.where(cache.k_tail != 0, 2.0 ** keys, 0.0))
         q = (base.float() * 2.0 ** e).to(torch.bfloat16) if e != 125 else (base.float().clamp(-3.98, 3.98) * 2.0 ** 126).to(torch.bfloat16)
+        q = torch.where(q.abs() < 2.0 ** -126, torch.zeros_like(q), q)         # (numbers with all their bits only)
         out, lse, _ = L.verify_attn_paged_mx(q, cache, i32(table), i32(kv), scale=scale, return_lse=True)
         ro, rl, _, size = M.attention(q.double().cpu().numpy(), M.as_numpy(cache), table, kv, None, scale if scale > 0 else None)
         o = out.double().cpu().numpy()
@@ -319,6 +322,8 @@ def test_queries_of_any_size(L, spare_cols):  # noqa: F811
         # a score off by d moves a probability by its d-th part: 2^-12, beside the two roundings to bf16
         assert np.all(np.abs(o - ro) <= (1.02 * 2.0 ** -8 + 2.0 ** -11) * (size + np.abs(ro)) + 1e-30), e
         assert np.all(np.abs(lse.cpu().numpy() - rl) <= 2.0 ** -12 + 2e-5 * (1 + np.abs(rl))), e
+    cache.k_scale.fill_(127)
+    cache.k_tail.copy_((cache.k_tail != 0).to(torch.bfloat16))
     want, wl, _ = L.verify_attn_paged_mx(base, cache, i32(table), i32(kv), return_lse=True)
     for value in (float("nan"), float("inf"), float("-inf")):
         q = base.clone()
@@ -339,6 +344,29 @@ def test_attention_over_the_largest_values(L):  # noqa: F811
     L.paged_mx_append(cache, torch.zeros_like(rows), rows, plan)
     out = L.verify_attn_paged_mx(torch.ones((1, 1, 1, D), dtype=torch.bfloat16, device=DEV), cache, i32([[0]]), i32([T]))
     assert bool((out.abs() <= 2.0 ** 128 * 1e-6).all())
+
+
+@pytest.mark.parametrize("spare_cols", [1, 70])
+@pytest.mark.parametrize("step", [1, 2, 7, 9])
+def test_large_values_where_scores_rise(L, step, spare_cols):  # noqa: F811
+    """One key of every tile has a score, from eight tiles to the next `step` (in base 2) higher, and the value 2^121; the
+    others are 2^300 below.  No weight is above 1 at any time, so sums of 41 are finite, and the output is 2^121."""
+    H, tiles = 128, 40
+    cache, table = ready_mx(L, 990, 1, H, [T * tiles], spare_cols=spare_cols)
+    for x in (cache.k_pool, cache.v_pool, cache.k_tail, cache.v_tail):
+        x.zero_()
+    cache.k_scale.fill_(127)
+    cache.v_scale.fill_(127 + 121)
+    cache.k_pool[:, :, 0, 1:, 0] = 0x0F                                        # channel 0: -6, of token 0: 0
+    cache.k_tail[..., 0] = -6.0
+    for j, block in enumerate(table[0][:tiles].tolist()):
+        cache.k_pool[block, :, 0, 0, 1] = (0, 2, 4, 5, 6)[j // 8]              # channel 2: 0 1 2 3 4
+        cache.v_pool[block, :, :, 0] = 0x02                                    # token 0: 1
+    q = torch.zeros((1, 1, 2 * H, D))
+    q[..., 0], q[..., 2] = 64.0, step
+    out = L.verify_attn_paged_mx(q.to(DEV, torch.bfloat16), cache, i32(table), i32([T * tiles]), scale=float(np.log(2.0)))
+    # probabilities and the output rounded to bf16
+    assert bool(((out.double() - 2.0 ** 121).abs() <= 2.0 ** 121 * 1.02 * 2.0 ** -7).all())
 
 
 def test_attention_is_the_same_every_time_and_on_streams(L):  # noqa: F811
