@@ -282,7 +282,10 @@ struct RotaryCallArgs {
   int D, in_place;
   int pieces, heads;            // pieces of a row, heads of a thread (of the launch)
 };
-constexpr int kRotaryEnough = 1 << 17;      // threads that fill the chip
+// Threads that fill the chip: a call with fewer splits its heads.  As many as these, half of them, twice: 300 rows, 40 + 8
+// heads of 128 in bf16 5.2, 4.6 and 5.2 us; 1500 rows 10.7, 10.2 and 11.5; 5000 rows 26.1, 29.7 and 26.7; 5001 rows of 32
+// heads of 80 in fp32 27.1, 29.6 and 25.9.
+constexpr int kRotaryEnough = 1 << 18;
 hipError_t launch_rotary(const RotaryCallArgs& a, int dtype, hipStream_t stream);
 
 struct AppendRotaryKernelArgs {
