@@ -581,8 +581,8 @@ typedef struct {
 int lvspec_paged_append_rotary(const lvspec_paged_append_rotary_args* args, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
- * Paged KV cache in 4 bits, in groups of 32 with a scale ("mx"): as the one in 8 bits, by the same plans, tables, slots and rings, with a complete block
- * in 8704 bytes a kv head instead of 16392.  Codes are e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign) and 32 values
+ * Paged KV cache in 4 bits, in groups of 32 with a scale ("mx"): as the one in 8 bits, by the same plans, tables,
+ * slots and rings, with a complete block in 8704 bytes a kv head instead of 16392.  Codes are e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign) and 32 values
  * share a scale, a power of two held as its exponent + 127 in a byte: of a key 32 channels of a token, of the values
  * 32 tokens of a channel.  value = code * scale; the scale is the smallest power of two s >= 2^-60 with max |x| <= 7 s,
  * so that no value is further from its code's than half a step there (codes end at 6, the next would be 8); codes
@@ -642,7 +642,10 @@ typedef struct {
 
 int lvspec_paged_mx_read(const lvspec_paged_mx_read_args* args, void* stream);
 
-/* Verification attention, as lvspec_verify_attn_paged. */
+/* Verification attention, as lvspec_verify_attn_paged.  Keys meet queries as they are in the cache; a query goes into that
+ * product as a sum of three numbers of 6 bits with a scale per 32 channels, from which it differs by at most 2^-15 of the
+ * largest of those (not at all where it is within 2^-7 of that; numbers below 2^-118 lose more).  32 channels of a query
+ * of which one is not finite make its row NaN. */
 typedef struct {
   lvspec_paged_mx_cache cache;
   int32_t gamma, Hq;                /* Hq % Hkv == 0; 1 <= gamma <= 32 */

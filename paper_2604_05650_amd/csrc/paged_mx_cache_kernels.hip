@@ -6,11 +6,14 @@ namespace lvspec {
 
 namespace {
 
+// 16384 rows of 8 heads 18.1 us, 85 MB at 4.7 TB/s (in 8 bits 20.4, 101 MB); 16 x 5 rows 3.0.
 __global__ __launch_bounds__(kCacheThreads) void paged_mx_append_kernel(AppendKernelArgs a) {
   __shared__ Pool4::Scratch scratch;
   append_rows<Pool4>(a, scratch, blockIdx.x, blockIdx.y, blockIdx.z != 0);
 }
 
+// 64 layers of 8 heads: one sequence's block completed in each 7.8 us, mostly launch and lengths; 16 sequences' second
+// chain of ten kept, four of whose blocks it completes, 38.7 (in 8 bits 8.4 and 41.9).
 template <bool PLANNED>
 __global__ __launch_bounds__(kCacheThreads) void paged_mx_commit_kernel(PagedCommitKernelArgs a) {
   __shared__ Pool4::Scratch scratch;
@@ -19,7 +22,8 @@ __global__ __launch_bounds__(kCacheThreads) void paged_mx_commit_kernel(PagedCom
 
 // ------------------------------------------------------------------------------ read
 // One workgroup per 64 packed rows, kv head and tensor.  A key's eight channels are a dword of its block; the values,
-// which lie by channel, go through LDS block by block.
+// which lie by channel, go through LDS block by block.  Bound by memory, most of it writes: 16384 rows of 8 heads 16.0 us,
+// 85 MB at 5.3 TB/s, 12 x (300 to 9000) rows 29.8 us, 179 MB at 6.0.
 __global__ __launch_bounds__(kCacheThreads) void paged_mx_read_kernel(ReadKernelArgs a) {
   __shared__ __align__(16) uint8_t s_codes[16 * 272];
   __shared__ __align__(16) uint8_t s_scale[kScale4Bytes];

@@ -1,4 +1,8 @@
 // Complete blocks of the paged cache in 4 bits (paged_mx_dev.h): rounding and layout.
+//
+// Keys are rounded where they are, eight channels of a token in a dword, and go to memory from there; the largest
+// magnitudes of values, whose groups run over tokens, and their codes, which lie by channel, go through LDS.  A row is read
+// once and a block written once: bound by memory as in 8 bits, of whose blocks these are half.
 #pragma once
 
 #include "paged_mx_dev.h"

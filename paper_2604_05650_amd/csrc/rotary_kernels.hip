@@ -1,7 +1,10 @@
 // Rotary positions: query and key rows turned by their positions.
 //
 // A thread has a piece of a row, W pairs of channels, in some of the row's heads: its cosines and sines are taken once
-// and serve all of them from registers.
+// and serve all of them from registers.  Every row is read once and written once: bound by memory where rows are many,
+// 16384 rows of 40 + 8 heads of 128 in bf16 83.6 us, 403 MB at 4.8 TB/s of the 5.1 that a large copy reaches; 5001 rows of 32
+// heads of 80 in fp32 26.9 us, 102 MB at 3.8, as long as a launch's start and end are in it.  80 rows take the 3.6 us of a
+// launch behind another.
 #include "rotary_dev.h"
 
 namespace lvspec {
