@@ -292,6 +292,28 @@ def test_scores_far_below_any_usual_one(L, n, spare_cols):  # noqa: F811
 
 
 @pytest.mark.parametrize("spare_cols", [1, 70])
+@pytest.mark.parametrize("power", [23, 30, 45, 113])
+def test_scores_far_from_usual_ones(L, power, spare_cols):  # noqa: F811
+    """Scores of all sizes up to 2^power, times a scale that binary32 does not hold, so that no maximum is exact: the row is the
+    mean of the values of its largest score (equal scores have equal weights, the others are far below)."""
+    n, H, rows = 64 * 21 + 5, 2, 3
+    cache, table = ready_mx(L, 940 + power, 1, H, [n], spare_cols=spare_cols)
+    rng = np.random.default_rng(power)
+    for x in (cache.k_pool, cache.k_tail):
+        x.zero_()
+    cache.k_scale.fill_(127)
+    code = torch.from_numpy(rng.integers(0, 8, (cache.k_pool.shape[0], H, T)).astype(np.uint8)).to(DEV)
+    cache.k_pool[:, :, 0, :, 1] = code << 4                                    # channel 3
+    cache.k_tail[..., 3] = torch.from_numpy(rng.integers(0, 7, (1, H, RING)).astype(np.float32)).to(DEV)
+    q = torch.zeros((1, 1, rows * H, D))
+    q[..., 3] = torch.tensor([1.0, -1.0, 1.375] * H) * 2.0 ** (power - 3)
+    out, lse, _ = L.verify_attn_paged_mx(q.to(DEV, torch.bfloat16), cache, i32(table), i32([n]), scale=0.7, return_lse=True)
+    ro, rl, _, size = M.attention(q.double().numpy(), M.as_numpy(cache), table, [n], None, float(np.float32(0.7)))
+    assert np.all(np.abs(out.double().cpu().numpy() - ro) <= 1.02 * 2.0 ** -8 * (size + np.abs(ro)))
+    assert np.all(np.abs(lse.double().cpu().numpy() - rl) <= 2e-5 * (1 + np.abs(rl)))
+
+
+@pytest.mark.parametrize("spare_cols", [1, 70])
 def test_queries_of_any_size(L, spare_cols):  # noqa: F811
     """Rows from bf16's smallest to its largest numbers, with channels of every size beside each other, where the score
     scale brings them back; and a row that is not finite is NaN, the others are what they are without it.
