@@ -880,6 +880,7 @@ _ROTARY_TYPES = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}
 def _fill_rotation(r: Rotation, rot: Rotary, pos, n_rows, transpose=False):
     inv = rot.inv_freq
     half = inv.numel()
+    assert half > 0
     r.dim, r.interleaved, r.transpose = 2 * half, 1 if rot.interleaved else 0, 1 if transpose else 0
     r.inv_freq = _dense(inv, torch.float32, (half,))
     r.axis = None if rot.axis is None else _dense(rot.axis, torch.uint8, (half,))
@@ -904,7 +905,7 @@ def _rows_of(x, dtype, n_rows):
 def _fill_queries(a, q, q_out, n_rows):
     a.Hq = 0
     if q is not None:
-        assert q_out is not None and q_out.shape == q.shape
+        assert q_out is not None and q_out.shape == q.shape and q.shape[2] == 128
         a.Hq = q.shape[1]
         a.q, a.q_sr, a.q_sh = _rows_of(q, torch.bfloat16, n_rows)
         a.q_out, a.qo_sr, a.qo_sh = _rows_of(q_out, torch.bfloat16, n_rows)

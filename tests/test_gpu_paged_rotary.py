@@ -177,3 +177,24 @@ def test_without_a_rotation_nothing_changes(L):  # noqa: F811
             L.paged_mx_append(made[0], k, v, plan)
             L.paged_mx_append(made[1], k, v, plan, rot=rot, pos=pos)
         assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(*made))
+
+
+def test_calls_that_are_refused(L):  # noqa: F811
+    """No frequencies, queries of other heads than the cache's, rows short of positions: before any launch."""
+    k, q = normal(1, (6, 2, D)), normal(2, (6, 4, D))
+    st = L.alloc_paged_state(1, 4, 4, DEV)
+    plan = L.paged_plan(i32([0]), i32([6]), st["held"], st["queue"], st["state"], st["table"], max_rows=6)
+    rot, _ = rotation(L, 0)
+    none = L.Rotary(torch.empty(0, device=DEV))
+    for bits in (8, 4):
+        cache = (L.alloc_paged_cache if bits == 8 else L.alloc_paged_mx_cache)(1, 2, 4, DEV)
+        for r, pos, queries, out in ((none, None, None, None), (rot, None, q[..., :64], q[..., :64]),
+                                     (rot, None, q[:5], torch.zeros_like(q[:5])), (rot, i32([0] * 5), None, None),
+                                     (rot, i32([[0] * 6] * 2), None, None), (rot, None, q.float(), q.float())):
+            with pytest.raises(AssertionError):
+                if bits == 8:
+                    L.paged_append_rotary(cache, k, k, plan, r, pos=pos, q=queries, q_out=out)
+                else:
+                    L.paged_mx_append(cache, k, k, plan, rot=r, pos=pos, q=queries, q_out=out)
+        torch.cuda.synchronize()
+        assert all(not bool(x.view(torch.uint8).any()) for x in cache)
