@@ -628,8 +628,14 @@ struct Segment {
     return rows;
   }
 
-  // open rows: positions L / 64 * 64 .. L + gamma - 1, in pieces of 32 keys, one stream each
+  // open rows: positions L / 64 * 64 .. L + gamma - 1, in pieces of 32 keys, one stream each (at most 95 rows, three pieces).
+  // `meet` is called when the stream's loads are on their way.
+  LVS_DEV bool has_open(int L) const { return (KS - 1 - stream) * 32 < (L & (kPageTokens - 1)) + p.gamma; }
   LVS_DEV void open_rows(int b, int h, int rc, int L) {
+    open_rows(b, h, rc, L, [] {});
+  }
+  template <class Meet>
+  LVS_DEV void open_rows(int b, int h, int rc, int L, Meet&& meet) {
     const int lane = lane_now(), n16 = lane & 15, g4 = lane >> 4;
     const int base = L & ~(kPageTokens - 1);
     const int n = L - base + p.gamma;
@@ -647,6 +653,7 @@ struct Segment {
 #pragma unroll
       for (int x = 0; x < 8; ++x)
         v[x] = *reinterpret_cast<const u32x4*>(vt + ((p0 + 4 * x + g4) & (kTailRows - 1)) * kRowBytes + n16 * 16);
+      meet();
       // Rows behind the last draft are nobody's: zero.  A value that is not finite would reach rows that do
       // not see its key, as 0 * inf: it is zero here as well, and its rows are remembered for below.
       uint32_t odd = 0;
