@@ -187,7 +187,7 @@ hipError_t launch_paged_attn(const PagedAttnKernelArgs& a, hipStream_t stream) {
   const bool once = a.n_rc == 1;
   const int64_t units = (int64_t)a.B * a.Hkv * a.n_rc;
   const int64_t cus = a.limit - units + 1;
-  if (a.cols <= unit_columns(a.B, units, cus)) {
+  if (a.cols <= unit_columns(a.B, units, cus, 18)) {
     if (a.rpad <= 16) return launch_units<Rows16, 8, true>(a, stream);      // (one chunk: two have 17 rows each and more)
     return once ? launch_units<WideRows, 8, true>(a, stream) : launch_units<WideRows, 8, false>(a, stream);
   }

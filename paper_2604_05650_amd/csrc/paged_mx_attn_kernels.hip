@@ -171,6 +171,9 @@ struct FourRows : WideRows {
   }
 };
 
+// What a call reads once is not left in the caches, which pays where it comes from memory, as over a model's layers, and costs
+// where the cache before the memory has it: 16384 keys, 25 rows over 30 sets 15.2 us and 15.9 without, over three 15.0 and
+// 14.5; 16 x (2048 to 32768) keys 47.6 and 51.2, 64 x 4000 57.0 and 61.5.
 template <bool ONCE, class T>
 LVS_DEV T load_once(const uint8_t* at) {
   const T* p = reinterpret_cast<const T*>(at);
@@ -324,7 +327,10 @@ hipError_t launch_paged_mx_attn(const PagedAttnKernelArgs& a, hipStream_t stream
   const bool once = a.n_rc == 1;
   const int64_t units = (int64_t)a.B * a.Hkv * a.n_rc;
   const int64_t cus = a.limit - units + 1;
-  if (a.cols <= unit_columns(a.B, units, cus))
+  // One workgroup per unit and parts, us: 8 units 800 keys 10.2 and 11.9, 1400 11.4 and 12.1, 2000 12.7 and 12.3; 64 units 1500
+  // keys 13.1 and 14.1, 2500 15.1 and 15.4, 4000 20.2 and 18.0; 128 units 2000 keys 14.2 and 18.6, 4000 21.1 and 22.9, 6000 27.7
+  // and 28.0; 256 units 4000 keys 29.2 and 32.4, 512 units 56.7 and 62.1.
+  if (a.cols <= unit_columns(a.B, units, cus, 26))
     return once ? launch_units4<8, true>(a, stream) : launch_units4<8, false>(a, stream);
   return once ? launch_parts4<8, true>(a, stream) : launch_parts4<8, false>(a, stream);
 }

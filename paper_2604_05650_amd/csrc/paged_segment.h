@@ -847,8 +847,9 @@ LVS_DEV bool find_part(const PagedAttnKernelArgs& p, Part& o) {
 // More than 64 kPer sequences are not cut, whose places a wave cannot hold.  That costs little where lengths are alike,
 // 250 x (400 to 12000) keys, 2 heads 96 and 92, and much where one sequence is far longer than the others: one of
 // 65536 keys among 500 each, 8 heads, 1 row of 5 heads 176 us with 256 sequences and 308 with 257.
-inline int unit_columns(int64_t B, int64_t units, int64_t cus) {
-  return B > 64 * kPer ? 1 << 30 : units >= cus / 2 ? 64 : 18;
+// `few`: the columns where units are fewer than half of the compute units.
+inline int unit_columns(int64_t B, int64_t units, int64_t cus, int few) {
+  return B > 64 * kPer ? 1 << 30 : units >= cus / 2 ? 64 : few;
 }
 
 }  // namespace
