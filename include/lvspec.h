@@ -564,7 +564,7 @@ int lvspec_rotary_frequencies(const lvspec_rotary_freq_args* args, float* inv_fr
  * lvspec_paged_append with the keys rotated on the way, and the rows' queries beside them in the same launch.  A
  * rotated key is rounded to bf16, as the ring holds it, before its block is rounded to 8 bits.  pos = NULL: rows are
  * turned by rows.row_pos, their places in the cache (n_axes 1).  Rows with row_seq < 0 have no query: theirs is left
- * as it is in q_out.
+ * as it is in q_out.  Without rows (n_rows 0) nothing is read, and q, q_out and pos may be NULL.
  * Errors: as lvspec_paged_append and lvspec_rotary; LVSPEC_EUNSUPPORTED for dim % 16 != 0, and for more than 2^24
  * workgroups, n_rows * Hkv / 32 + n_rows / 32; LVSPEC_EINVAL for transpose.
  * ------------------------------------------------------------------------------------------- */

@@ -38,9 +38,10 @@ template <class Args>
 int fill_append_rotation(const Args* a, const lvspec::AppendKernelArgs& rows, lvspec::AppendRotaryKernelArgs& k) {
   int rc = fill_rotation(a->rot, LVSPEC_HEAD_DIM, k.rot);
   if (rc != LVSPEC_OK) return rc;
-  if (a->rot.transpose != 0 || a->Hq < 0 || (a->rot.pos == nullptr && a->rot.n_axes != 1)) return LVSPEC_EINVAL;
+  const bool any = rows.n_rows > 0;          // (without rows there are no positions and no queries to point at)
+  if (a->rot.transpose != 0 || a->Hq < 0 || (any && a->rot.pos == nullptr && a->rot.n_axes != 1)) return LVSPEC_EINVAL;
   if (a->rot.dim % 16 != 0 || a->Hq > 65535) return LVSPEC_EUNSUPPORTED;
-  if (a->Hq > 0) {
+  if (any && a->Hq > 0) {
     rc = fill_rows(a->Hq, LVSPEC_HEAD_DIM, LVSPEC_BF16, a->q, a->q_sr, a->q_sh, a->q_out, a->qo_sr, a->qo_sh, k.q);
     if (rc != LVSPEC_OK) return rc;
   }
