@@ -59,9 +59,13 @@ struct Turn {
     }
   }
   // Pair j: a[j] and b[j], or (`pairs`) neighbours of the 2 W channels a, b.  The sums are in 64 bits, rounded to
-  // binary32 and then to the rows' type.
+  // binary32 and then to the rows' type, in every channel and every call alike, since a key's codes go by it.  (Left to
+  // itself the compiler takes the two roundings as one where both stand in one basic block, one channel in 8 of rows and
+  // one in 16 of appends, and about one number in 2^17 is another there.  Rounded once, that one would be nearer by up to
+  // 2^-17 of a step of bf16; but no instruction rounds 64 bits to bf16, and every number would take several.)
   LVS_DEV void apply(float (&a)[W], float (&b)[W], bool pairs) const {
     auto one = [&](float& x, float& y, int j) {
+#pragma clang fp contract(off)
       const double u = x, v = y;
       x = (float)__builtin_fma(u, c[j], -(v * s[j]));
       y = (float)__builtin_fma(v, c[j], u * s[j]);
