@@ -506,6 +506,8 @@ int lvspec_paged_commit(const lvspec_paged_commit_args* args, void* stream);
  * channel and by every call that rotates alike (of two roundings about one bf16 number in 2^17 is not the nearest).
  * Where frequencies are stretched for long contexts, inv_freq and factor say how (lvspec_rotary_frequencies).
  * Rows may be turned in place (out = in, with the same strides) and must not overlap otherwise.
+ * Pointers and strides of rows and heads are multiples of 16 bytes, strides no less than D: heads of other sizes lie in
+ * wider ones, whose rest is not touched.
  * Errors: LVSPEC_EINVAL for NULL / misaligned / out-of-range arguments, LVSPEC_EUNSUPPORTED for D > 512, more than
  * 65535 heads or 2^32 row channels (n_rows * D).
  * ------------------------------------------------------------------------------------------- */

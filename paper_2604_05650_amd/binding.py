@@ -902,6 +902,15 @@ def _rows_of(x, dtype, n_rows):
     return x.data_ptr(), x.stride(0) if n > 1 else max(most, H * most), x.stride(1) if H > 1 else most
 
 
+def _new_rows(x):
+    """Uninitialised rows of x's shape as _rows_of wants them: every head from one 16-byte border to the next."""
+    n, H, D = x.shape
+    per = 16 // x.element_size()
+    if D % per == 0:
+        return torch.empty_like(x, memory_format=torch.contiguous_format)
+    return torch.empty((n, H, -(-D // per) * per), dtype=x.dtype, device=x.device)[..., :D]
+
+
 def _fill_queries(a, q, q_out, n_rows):
     a.Hq = 0
     if q is not None:
@@ -932,11 +941,12 @@ def rotary_args(q, pos, rot: Rotary, *, out, k=None, k_out=None, transpose=False
 def rotary(q, pos, rot: Rotary, *, k=None, out=None, k_out=None, transpose=False, stream=None):
     """lvspec_rotary.  q [n_rows,Hq,D] and k [n_rows,Hkv,D] (optional) bf16, fp16 or fp32; pos int32 [n_rows], or
     [n_axes,n_rows] with rot.axis.  out and k_out may be q and k.  transpose: turned back, the gradient of q (and k)
-    from that of out.  Returns out, or (out, k_out)."""
+    from that of out.  Returns out, or (out, k_out).  Rows and heads start on 16-byte borders, so heads of other sizes are
+    slices of wider ones; what is allocated here is, and contiguous where heads are whole multiples of 16 bytes."""
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        out = _new_rows(q)
     if k is not None and k_out is None:
-        k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
+        k_out = _new_rows(k)
     a = rotary_args(q, pos, rot, out=out, k=k, k_out=k_out, transpose=transpose)
     _call_on(q.device, _lib.lvspec_rotary, a, stream)
     return out if k is None else (out, k_out)
