@@ -645,10 +645,12 @@ typedef struct {
 
 int lvspec_paged_mx_read(const lvspec_paged_mx_read_args* args, void* stream);
 
-/* Verification attention, as lvspec_verify_attn_paged.  Keys meet queries as they are in the cache; a query goes into that
- * product as a sum of three numbers of 6 bits with a scale per 32 channels, from which it differs by at most 2^-15 of the
- * largest of those (not at all where it is within 2^-7 of that; numbers below 2^-118 lose more).  32 channels of a query
- * of which one is not finite make its row NaN. */
+/* Verification attention, as lvspec_verify_attn_paged.  Keys of complete blocks meet queries as they are in the cache; a
+ * query goes into that product as a sum of three numbers of 6 bits with a scale per 32 channels.  Channels of 1/64 of the
+ * largest of their 32 and above lose nothing, smaller ones differ by at most 2^-14.9 of that largest (or 2^-131, where that
+ * is more: a largest below 2^-116, which loses up to 2^-131 too).  32 channels of a query of which one is not finite make
+ * its row NaN.  The open rows' keys meet queries as they are, and so does all of the cache in 8 bits, for queries whose
+ * channels differ by more than that allows. */
 typedef struct {
   lvspec_paged_mx_cache cache;
   int32_t gamma, Hq;                /* Hq % Hkv == 0; 1 <= gamma <= 32 */

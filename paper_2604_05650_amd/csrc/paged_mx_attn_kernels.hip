@@ -5,8 +5,8 @@
 // them: they are loaded straight into registers, 1 KiB in one piece per instruction.
 //   S^T = K Q^T: keys go into the matrix instructions as they are, with their scales.  What they meet are sums of three
 //     numbers of 6 bits (e2m3, 1 to 7.5 in steps of an eighth to a half, and down to an eighth) with a power of two per
-//     row and 32 channels: of a bf16 number within 2^-7 of the largest of its 32 nothing is lost, of a smaller one at
-//     most 2^-15 of that largest.  12 instructions of half the time instead of 16 of bf16, and no keys to widen.
+//     row and 32 channels: a bf16 number of 1/64 of the largest of its 32 and above loses nothing, a smaller one at
+//     most 2^-14.9 of that largest (split6).  12 instructions of half the time instead of 16 of bf16, and no keys to widen.
 //   O^T = V^T P^T: scores are left in the lanes that hold the values of their tokens, so probabilities, rounded to bf16
 //     (each by at most 2^-8 of itself), go into the second product where they are; values are widened to bf16 with
 //     their scales (exact).  In numbers of 6 bits probabilities take three as well, whose making costs what the
@@ -46,7 +46,9 @@ LVS_DEV f32x32 from_six(const Six& x, float scale) {
 }
 
 // Three terms, at scales of 1, 2^-4 and 2^-9, of numbers up to 7.5: what a term leaves, at most a quarter of its scale, is
-// at most 4 of the second's, and what that leaves, an eighth, at most 4 of the third's.
+// at most 4 of the second's, and what that leaves, an eighth, at most 4 of the third's.  Of a bf16 number the first two leave
+// no more than 2^-8, 2 of the third's scale, where its step is 2^-12: numbers from 2^-5 on, whose last bit that is, are exact,
+// and smaller ones off by 2^-13 at most.  The largest of the 32 is above 3.75, so that is 2^-14.9 of it.
 template <class Put>
 LVS_DEV void split6(f32x16 x, f32x16 y, Put&& put) {
   constexpr float kScale[3] = {1.f, 0x1p-4f, 0x1p-9f};
