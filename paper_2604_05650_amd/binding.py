@@ -867,6 +867,8 @@ class Rotary(NamedTuple):
 def rotary_frequencies(dim, base=10000.0, *, scaling=SCALING_NONE, scale=1.0, original_len=0, beta_fast=0.0, beta_slow=0.0,
                        device=None):
     """lvspec_rotary_frequencies: (inv_freq fp32 [dim / 2] on `device`, factor)."""
+    if not 0 < dim <= 512:                     # (before 32 bits are taken of it)
+        raise LvspecError(EINVAL)
     a = RotaryFreqArgs(int(dim), int(scaling), float(base), float(scale), float(original_len), float(beta_fast),
                        float(beta_slow))
     out, factor = (C.c_float * max(1, int(dim) // 2))(), C.c_float()
@@ -922,8 +924,9 @@ def _fill_queries(a, q, q_out, n_rows):
 
 def rotary_args(q, pos, rot: Rotary, *, out, k=None, k_out=None, transpose=False) -> RotaryArgs:
     a = RotaryArgs()
-    _one_device(q, pos, out, k, k_out, rot.inv_freq, rot.axis)
     n, Hq, D = q.shape
+    assert n < 1 << 31, f"{n} rows"            # (the field would take 32 bits of it)
+    _one_device(q, pos, out, k, k_out, rot.inv_freq, rot.axis)
     _fill_rotation(a.rot, rot, pos, n, transpose)
     a.n_rows, a.Hq, a.Hkv, a.D, a.dtype = n, Hq, 0, D, _ROTARY_TYPES[q.dtype]
     assert out.shape == q.shape
