@@ -501,8 +501,8 @@ int lvspec_paged_commit(const lvspec_paged_commit_args* args, void* stream);
  *     a = pos[axis[i], t] * inv_freq[i]         c = factor cos a      s = factor sin a
  *     y1 = x1 c - x2 s,  y2 = x2 c + x1 s       (x1, x2): channels i, i + dim/2, interleaved 2 i, 2 i + 1
  * transpose = 1 turns back (s negative), the gradient of x from that of y.  A token of a video has a position
- * on several axes (time, height, width), and a frequency goes by one of them.  Angles, their cosines and
- * sines, and the two products are in 64 bits; the result is rounded to binary32 and then to the rows' type, in every
+ * on several axes (time, height, width), and a frequency goes by one of them.  Angles (below 2^48), their
+ * cosines and sines, and the two products are in 64 bits; the result is rounded to binary32 and then to the rows' type, in every
  * channel and by every call that rotates alike (of two roundings about one bf16 number in 2^17 is not the nearest).
  * Where frequencies are stretched for long contexts, inv_freq and factor say how (lvspec_rotary_frequencies).
  * Rows may be turned in place (out = in, with the same strides) and must not overlap otherwise.
@@ -522,7 +522,7 @@ typedef struct {
   const uint8_t* axis;              /* DEVICE [dim / 2], each below n_axes (else the last); NULL: the first */
   const int32_t* pos;               /* DEVICE [n_axes, n_rows] */
   int64_t pos_sa;                   /* stride of pos: axis */
-  float factor;                     /* of cosines and sines, > 0; 0 = 1 */
+  float factor;                     /* of cosines and sines, > 0 and <= 10^6; 0 = 1 */
 } lvspec_rotation;
 
 typedef struct {

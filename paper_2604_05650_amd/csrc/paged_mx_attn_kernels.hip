@@ -79,8 +79,9 @@ LVS_DEV f32x16 mfma_mx(const u32x4& a, uint32_t ks, const Six& b, uint32_t qs, c
 // 32 t + 8 (r / 4) + 4 h + r % 4.
 struct FourRows : WideRows {
   // A row of 32 tiles meets a new maximum in most of them, if only by a little, and a rescaling is a fifth of a tile's
-  // vector instructions: 4 x 65536 keys, 64 rows 87.4 -> 81.6 us, 16 x (2048 to 32768) keys 51.0 -> 48.5.  (The exact 1
-  // that the largest probability often is otherwise is lost.)
+  // vector instructions: 4 x 65536 keys, 64 rows 87.4 -> 81.6 us, 16 x (2048 to 32768) keys 51.0 -> 48.5.  The exact 1
+  // that the largest probability often is otherwise is lost, and its rounding is one more: error against 64 bits 2.1e-3 and
+  // 2.0e-3 -> 2.3e-3 (every probability is within 2^-8 of itself either way).
   static constexpr int kSlack = 8;
   static LVS_DEV int key_of(int lane, int e) { return 32 * (e >> 4) + 8 * ((e >> 2) & 3) + 4 * (lane >> 5) + (e & 3); }
   // channels 64 a + 32 h + 8 y .. +7 at 4 a + y, of queries and of open keys

@@ -5,7 +5,9 @@
 // hide behind the loads in part: vector instructions take 47 % of the time), 12 x (300 to 9000) rows of 4 heads with 28 of
 // queries 114 us, 535 MB at 4.7; into the one in 4 bits 12 x (300 to 9000) rows of 8 heads 52 us, 161 MB at 3.1.  By what
 // follows what where they are few: 16 x 5 rows 7.1 us (4.3 without the rotation), 2048 rows into 4 bits 12: places,
-// requests, rows and positions one behind the other, then 16 angles of a thread.
+// requests, rows and positions one behind the other, then 16 angles of a thread.  Where rows are many, two workgroups a
+// compute unit are all that 213 (8 bits) and 219 (4 bits) registers leave room for, 64 of them the cosines and sines of a
+// thread's two rows.
 #include "paged_mx_store.h"
 #include "rotary_dev.h"
 
@@ -13,8 +15,9 @@ namespace lvspec {
 
 namespace {
 
-// The packed rows of a tile and the blocks that end in it, as append_rows finds them, with the requests' first rows asked
-// for by all lanes at once.
+// The packed rows of a tile and the blocks that end in it, as append_rows (paged_store.h) finds them for one head, with the
+// requests' first rows asked for by all lanes at once.  Both go by RowPlace for which ring rows are left to who reads the
+// request's open block (`later`), and write those behind its reads: a change to one is a change to both.
 struct Tile {
   const AppendKernelArgs& a;
   const int t0, lane;

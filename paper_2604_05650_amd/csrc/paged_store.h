@@ -137,7 +137,8 @@ struct RowPlace {
 // last row; its first rows may be the packed rows of the tiles before or, where they came in an earlier
 // call, rows of the ring.  Every row is read once and every block written once: bound by memory, 4.6 to 5.3 TB/s
 // of reads and writes (16384 rows, 8 heads 19 to 22 us, 12 x (300 to 9000) rows 41), where a torch copy reaches
-// 4.9; the turn of the values through LDS, a third of whose cycles are bank conflicts, hides behind that.
+// 4.9; the turn of the values through LDS, a third of whose cycles are bank conflicts, hides behind that.  (Appends that
+// rotate have this walk once more, for several heads: Tile of paged_rotary_kernels.hip.)
 template <class Pool>
 LVS_DEV void append_rows(const AppendKernelArgs& a, typename Pool::Scratch& scratch, int tile, int h, bool values) {
   const int tid = threadIdx.x, lane = tid & 63, q = tid >> 4, c = tid & 15;
