@@ -9,12 +9,12 @@ namespace lvspec {
 namespace {
 
 // Cosine and sine in 64 bits: the angle less a multiple of pi/2, taken off in two parts of pi/2 with one rounding
-// each, and Taylor's series on what is left, |x| <= pi/4, whose next terms are 2e-14 (9e-14 at angles of
-// 2^48).  In 64 bits because the angles of far positions need them (position 10^6 in 32 bits is 0.06 off), and because rows
-// that go into a cache of few bits stand on the borders between two codes: one in 60 bf16 numbers does, and a last bit that depends on how the
-// sine was taken would choose the code.  That costs nothing where memory bounds a call (16384 rows of keys into a cache 27.0
-// us, 25.6 with angles as they are in place of their sines) and one to two microseconds where latency does (16 x 5 rows 7.0
-// and 5.6, 2048 rows 17.4 and 15.6).
+// each, and Taylor's series on what is left, |x| <= pi/4, whose next terms are 2e-14 (9e-14 at angles of 2^48).  In 64
+// bits because the angles of far positions need them (position 10^6 in 32 bits is 0.06 off), and because rows that go into
+// a cache of few bits stand on the borders between two codes: one in 60 bf16 numbers does, and a last bit that depends on
+// how the sine was taken would choose the code.  That costs nothing where memory bounds a call (16384 rows of keys into a
+// cache 27.0 us, 25.6 with angles as they are in place of their sines) and one to two microseconds where latency does
+// (16 x 5 rows 7.0 and 5.6, 2048 rows 17.4 and 15.6).
 LVS_DEV void cos_sin(double a, double& c, double& s) {
   const double n = __builtin_rint(a * 0.63661977236758134308);                     // 2 / pi
   double x = __builtin_fma(-n, 1.57079632679489661923, a);                         // pi / 2, rounded
